@@ -9,7 +9,10 @@
  * be prefetched while attention runs (sections 4.1-4.2).  This library is the
  * data-parallel part of that: the predictor itself for many tokens and layers
  * at once, the per-expert grouping of its selections (the prefetch list), and
- * the accuracy counters of section 5.1.
+ * the accuracy counters of section 5.1.  Beside it stands what the same layer
+ * runs in a decode step while its experts are fetched and once they are there:
+ * attention of one new token over a paged key-value cache, the cache's upkeep,
+ * and the mixture-of-experts layer itself.
  *
  * Conventions for every entry point
  *   - Pointers named *_dev are DEVICE pointers owned by the caller (inputs,
@@ -356,6 +359,165 @@ paep_status paep_confidence_select(const int32_t *idx_dev, const float *probs_de
  */
 paep_status paep_activation_profile(const int32_t *counts_dev, int32_t L, int32_t E, int32_t *order_dev,
                                     int32_t *n_active_dev, double *entropy_dev, void *stream);
+
+/*
+ * ---- a layer's decode step beside the predictor: paged key-value cache, attention, expert layer ----
+ *
+ * A key-value cache of one layer: two pools of pages, shared by all sequences,
+ * and a page table per sequence.  Position p of sequence b is slot
+ * p % page_size of page table[b][p / page_size]; its keys of head h start at
+ *     k_pages + page*k_page_stride + h*k_head_stride + slot*k_slot_stride
+ * (strides in ELEMENTS, so that a page may hold its heads or its slots as the
+ * outer dimension), Dk elements in a row; the values likewise, Dv elements.
+ * Pool pointers and strides must be 16-byte aligned.  page_table_dev is
+ * [B][max_pages] int32.  An entry outside [0, n_pages) names no page: paep_attend
+ * leaves the positions on it out, the other calls neither read nor write them.
+ * lengths_dev is [B] int32; a length below 0 counts as 0, one above a call's
+ * max_len as max_len.
+ */
+typedef struct {
+    int32_t B;          /* sequences, >= 0 */
+    int32_t Hkv;        /* key-value heads, 1..PAEP_MAX_HEADS */
+    int32_t Dk;         /* width of a key, multiple of 8, 8..PAEP_MAX_HEAD_DIM */
+    int32_t Dv;         /* width of a value, likewise */
+    int32_t page_size;  /* positions per page, a power of two, 1..65536 */
+    int32_t n_pages;    /* pages in the pools, >= 1 */
+    int32_t max_pages;  /* entries of a sequence in the page table, >= 1 */
+    int32_t dtype;      /* paep_dtype of queries, keys, values and outputs */
+    int64_t k_page_stride, k_head_stride, k_slot_stride;
+    int64_t v_page_stride, v_head_stride, v_slot_stride;
+} paep_cache_desc;
+
+#define PAEP_MAX_HEADS 1024
+#define PAEP_MAX_HEAD_DIM 256
+
+typedef struct {
+    int32_t Hq;               /* query heads, a multiple of Hkv, <= PAEP_MAX_HEADS; heads h*Hq/Hkv .. share key-value head h */
+    int32_t max_len;          /* no length is above this: 0..max_pages*page_size.  The work is laid out for it */
+    float scale;              /* factor of the scores, finite (usually 1/sqrt(Dk)) */
+    int32_t reserved;         /* 0 */
+    int64_t q_seq_stride;     /* elements between the queries of two sequences ... */
+    int64_t q_head_stride;    /* ... and of two heads, both 16-byte aligned */
+    int64_t mass_stride;      /* floats between two heads' rows of mass, >= max_len (ignored without mass) */
+} paep_attend_desc;
+
+/* Bytes of device workspace paep_attend needs for this shape, with or without
+ * the mass output; 0 is possible, and the answer for an invalid descriptor. */
+size_t paep_attend_workspace_bytes(const paep_cache_desc *cache, const paep_attend_desc *desc, int32_t want_mass);
+
+/*
+ * Attention of one new token per sequence over the cache.  With G = Hq/Hkv,
+ * g = h/G and R_b = the positions p with start_b <= p < length_b:
+ *     s[b,h,p]   = scale * q[b,h] . k[b,g,p]                 p in R_b
+ *     P[b,h,p]   = exp(s[b,h,p] - max_p s) / sum_p exp(s[b,h,p] - max_p s)
+ *     out[b,h]   = sum_p P[b,h,p] v[b,g,p]                   rounded once to dtype
+ *     lse[b,h]   = ln sum_p exp(s[b,h,p])
+ *     mass[b,g,p] += sum over the G heads h of P[b,h,p]      p in R_b; all else stays
+ * Scores, softmax and sums are fp32.  Where R_b is empty (or every score is
+ * -infinity) out is 0, lse is -infinity and mass stays.
+ *   q_dev [B][Hq] rows of Dk elements, strides in desc;  out_dev [B][Hq][Dv]
+ *   starts_dev  [B] int32 or NULL (all 0): the first position looked at, for a
+ *               sliding window or padding on the left; below 0 counts as 0
+ *   lse_dev     [B][Hq] float or NULL
+ *   mass_dev    [B][Hkv][mass_stride] float or NULL: the accumulated attention
+ *               weight that paep_cache_evict goes by
+ *   workspace_dev: at least paep_attend_workspace_bytes, 16-byte aligned, may be
+ *               NULL when that is 0; contents on entry do not matter
+ * q and out must be 16-byte aligned.
+ */
+paep_status paep_attend(const paep_cache_desc *cache, const paep_attend_desc *desc, const void *q_dev,
+                        const void *k_pages_dev, const void *v_pages_dev, const int32_t *page_table_dev,
+                        const int32_t *lengths_dev, const int32_t *starts_dev,
+                        void *out_dev, float *lse_dev, float *mass_dev,
+                        void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/*
+ * Writes the keys and values of n tokens into the cache: row i goes to position
+ * positions[i] of sequence sequences[i] (of sequence i where sequences_dev is
+ * NULL; n <= B then).  Rows whose position is below 0 or at or above
+ * max_pages*page_size, whose sequence is outside [0, B) or whose page is none are
+ * skipped.  The pages must be there already; lengths are the caller's to advance.
+ * No two rows may name the same place.
+ *   k_dev [n] rows of Hkv keys (k_row_stride elements between two rows, heads Dk
+ *         apart), v_dev likewise: pointers and strides 16-byte aligned
+ *   mass_dev [B][Hkv][mass_stride] float or NULL: set to 0 at the positions
+ *         written that are below mass_stride
+ */
+paep_status paep_cache_append(const paep_cache_desc *cache, int32_t n, const void *k_dev, int64_t k_row_stride,
+                              const void *v_dev, int64_t v_row_stride, void *k_pages_dev, void *v_pages_dev,
+                              const int32_t *page_table_dev, const int32_t *sequences_dev, const int32_t *positions_dev,
+                              float *mass_dev, int64_t mass_stride, void *stream);
+
+/*
+ * Cuts every sequence down to at most `budget` positions: of a length n > budget
+ * each head keeps the last `recent` positions and, of those before them, the
+ * budget - recent with the largest mass (equal: the lower position; NaN is below
+ * every number, and both zeros are equal); of n <= budget it keeps all.  What is kept is
+ * copied, in ascending position, to positions 0, 1, ... on the pages of out_table
+ * (pages of the same pools), which must not be pages that any table entry of
+ * the sequences being read names.
+ *     kept[b,h,j]      the j-th kept position, -1 behind the last
+ *     mass_out[b,h,j]  mass[b,h,kept[b,h,j]], 0 behind the last, j < mass_out_stride
+ *     lengths_out[b]   min(n, budget)
+ * A kept position whose page (or new page) is none is not copied.
+ *   max_len 0..max_pages*page_size as in paep_attend, mass_stride >= max_len;
+ *   1 <= budget <= out_max_pages*page_size, 0 <= recent <= budget
+ *   out_table_dev [B][out_max_pages] int32, kept_dev [B][Hkv][budget] int32,
+ *   mass_dev [B][Hkv][mass_stride], mass_out_dev [B][Hkv][mass_out_stride] float
+ *   (another buffer, mass_out_stride >= min(budget, max_len)); lengths_out_dev [B] int32, not lengths_dev
+ */
+paep_status paep_cache_evict(const paep_cache_desc *cache, int32_t max_len, int32_t budget, int32_t recent,
+                             void *k_pages_dev, void *v_pages_dev, const int32_t *page_table_dev,
+                             const int32_t *lengths_dev, const float *mass_dev, int64_t mass_stride,
+                             const int32_t *out_table_dev, int32_t out_max_pages,
+                             int32_t *kept_dev, float *mass_out_dev, int64_t mass_out_stride, int32_t *lengths_out_dev,
+                             void *stream);
+
+/* Shape of a mixture-of-experts layer for a few tokens. */
+typedef struct {
+    int32_t T;          /* tokens, 0..PAEP_MOE_MAX_T */
+    int32_t d;          /* hidden size, multiple of 8, >= 8 */
+    int32_t f;          /* inner width of an expert, multiple of 8, >= 8 */
+    int32_t E;          /* experts, 1..PAEP_MAX_E */
+    int32_t k;          /* experts per token, 1..min(E, PAEP_MAX_K) */
+    int32_t dtype;      /* paep_dtype of x, the weights, residual and y */
+    int32_t act;        /* paep_act on the gate: NONE, SILU, GELU */
+    int32_t prob;       /* paep_prob: what weighs an expert's output */
+} paep_moe_desc;
+
+#define PAEP_MOE_MAX_T 64
+
+/* Bytes of device workspace that paep_moe_layer and paep_moe_experts need; 0 for an invalid descriptor. */
+size_t paep_moe_workspace_bytes(const paep_moe_desc *desc);
+
+/*
+ * The layer that the predictor predicts: router, selection, gated experts,
+ * weighted sum.  For every token t:
+ *     z = Wg x_t (+ bg), fp32;   idx[t] = the k highest of z, as in paep_predict
+ *     p[t,j] = the softmax of z at idx[t,j], or what prob says;  probs = p
+ *     u_j = W13[idx_j][0..f) x_t,   w_j = W13[idx_j][f..2f) x_t
+ *     h_j = p_j act(u_j) w_j              in bf16 storage held as two bf16 parts, 16 bits of it
+ *     y_t = residual_t + sum_j W2[idx_j] h_j        fp32 sums, rounded once to dtype
+ *   x_dev [T][d], Wg_dev [E][d], bg_dev [E] or NULL, W13_dev [E][2f][d] (the f
+ *   gate rows, then the f others), W2_dev [E][d][f], residual_dev [T][d] or NULL
+ *   y_dev [T][d] (may be residual_dev, not x_dev), idx_dev [T][k] int32, probs_dev [T][k] float
+ *   counts_dev [E] int32 or NULL: increased by the number of tokens per expert
+ * x, the weights, residual and y must be 16-byte aligned.
+ */
+paep_status paep_moe_layer(const paep_moe_desc *desc, const void *x_dev, const void *Wg_dev, const void *bg_dev,
+                           const void *W13_dev, const void *W2_dev, const void *residual_dev,
+                           void *y_dev, int32_t *idx_dev, float *probs_dev, int32_t *counts_dev,
+                           void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/*
+ * The same with a selection that is there already (another router's, or the
+ * predictor's own): idx_dev and probs_dev are read.  Ids outside [0, E) are
+ * skipped (the -1 that paep_confidence_select writes); one that stands in a row
+ * several times weighs the sum of its probabilities.  desc->prob is not looked at.
+ */
+paep_status paep_moe_experts(const paep_moe_desc *desc, const void *x_dev, const void *W13_dev, const void *W2_dev,
+                             const int32_t *idx_dev, const float *probs_dev, const void *residual_dev, void *y_dev,
+                             void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /*
  * Device ceilings, measured: not part of the paper's method.  The benchmark

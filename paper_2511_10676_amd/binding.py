@@ -39,7 +39,9 @@ EXPORTS = ["paep_predict_workspace_bytes", "paep_predict_workspace_min_bytes", "
            "paep_predict_counted", "paep_predict_confidence", "paep_fold_batchnorm",
            "paep_group_workspace_bytes", "paep_group_by_expert", "paep_score",
            "paep_score_rows", "paep_confidence_select", "paep_activation_profile", "paep_probe_read",
-           "paep_probe_mfma", "paep_status_string", "paep_version"]
+           "paep_probe_mfma", "paep_status_string", "paep_version",
+           "paep_attend_workspace_bytes", "paep_attend", "paep_cache_append", "paep_cache_evict",
+           "paep_moe_workspace_bytes", "paep_moe_layer", "paep_moe_experts"]
 
 
 class PredictDesc(ctypes.Structure):
@@ -49,6 +51,21 @@ class PredictDesc(ctypes.Structure):
                 ("prob", ctypes.c_int32),
                 ("x_layer_stride", ctypes.c_int64), ("w1_layer_stride", ctypes.c_int64),
                 ("w2_layer_stride", ctypes.c_int64)]
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hkv", "Dk", "Dv", "page_size", "n_pages", "max_pages", "dtype")] + \
+               [(n, ctypes.c_int64) for n in ("k_page_stride", "k_head_stride", "k_slot_stride",
+                                              "v_page_stride", "v_head_stride", "v_slot_stride")]
+
+
+class AttendDesc(ctypes.Structure):
+    _fields_ = [("Hq", ctypes.c_int32), ("max_len", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+                ("q_seq_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64), ("mass_stride", ctypes.c_int64)]
+
+
+class MoeDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "d", "f", "E", "k", "dtype", "act", "prob")]
 
 
 class PaepError(RuntimeError):
@@ -114,6 +131,21 @@ def lib() -> ctypes.CDLL:
         L.paep_probe_read.restype = ctypes.c_int
         L.paep_probe_mfma.argtypes = [i32, i32, vp, sz, vp, ctypes.POINTER(ctypes.c_double)]
         L.paep_probe_mfma.restype = ctypes.c_int
+        i64, cp, ap, mp = ctypes.c_int64, ctypes.POINTER(CacheDesc), ctypes.POINTER(AttendDesc), ctypes.POINTER(MoeDesc)
+        L.paep_attend_workspace_bytes.argtypes = [cp, ap, i32]
+        L.paep_attend_workspace_bytes.restype = sz
+        L.paep_attend.argtypes = [cp, ap] + [vp] * 10 + [sz, vp]
+        L.paep_attend.restype = ctypes.c_int
+        L.paep_cache_append.argtypes = [cp, i32, vp, i64, vp, i64] + [vp] * 6 + [i64, vp]
+        L.paep_cache_append.restype = ctypes.c_int
+        L.paep_cache_evict.argtypes = [cp, i32, i32, i32] + [vp] * 5 + [i64, vp, i32, vp, vp, i64, vp, vp]
+        L.paep_cache_evict.restype = ctypes.c_int
+        L.paep_moe_workspace_bytes.argtypes = [mp]
+        L.paep_moe_workspace_bytes.restype = sz
+        L.paep_moe_layer.argtypes = [mp] + [vp] * 11 + [sz, vp]
+        L.paep_moe_layer.restype = ctypes.c_int
+        L.paep_moe_experts.argtypes = [mp] + [vp] * 8 + [sz, vp]
+        L.paep_moe_experts.restype = ctypes.c_int
         L.paep_status_string.argtypes = [ctypes.c_int]
         L.paep_status_string.restype = ctypes.c_char_p
         L.paep_version.restype = ctypes.c_int
@@ -516,6 +548,263 @@ def fold_batchnorm(W1: torch.Tensor, b1: Optional[torch.Tensor], gamma: torch.Te
     if st != 0:
         raise PaepError(st, "paep_fold_batchnorm")
     return (W1o[0], b1o[0]) if squeeze else (W1o, b1o)
+
+
+# ---- a layer's decode step beside the predictor ----
+
+def _need_int32(dev, *named):
+    """Contiguous int32 tensors of the given shapes on `dev` (shape None: any; tensor None: left out)."""
+    for name, t, shape in named:
+        if t is None:
+            continue
+        if t.dtype != torch.int32 or t.device != dev or not t.is_contiguous() or (shape is not None and tuple(t.shape) != shape):
+            raise ValueError(f"{name} must be contiguous int32" + (f" {list(shape)}" if shape is not None else "") + " on the cache's device")
+
+
+def _need_rows(dev, dtype, *named):
+    """Tensors of the cache's type and device whose last dimension is contiguous."""
+    for name, t in named:
+        if t.dtype != dtype or t.device != dev or t.stride(-1) != 1:
+            raise ValueError(f"{name} must be of the cache's type and device, its last dimension contiguous")
+
+
+def _need_mass(dev, name, t, B, Hkv, least):
+    if t.dtype != torch.float32 or t.device != dev or not t.is_contiguous() or t.dim() != 3 or t.shape[0] != B \
+            or t.shape[1] != Hkv or t.shape[2] < least:
+        raise ValueError(f"{name} must be contiguous float32 [{B}, {Hkv}, at least {least}] on the cache's device")
+
+
+def _stride(t: torch.Tensor, dim: int) -> int:
+    """Stride of a dimension; 0 where it has one entry (torch leaves any value there)."""
+    return t.stride(dim) if t.shape[dim] > 1 else 0
+
+
+def _cache_desc(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor) -> CacheDesc:
+    """The cache k_pages [n_pages, Hkv, page_size, Dk], v_pages [n_pages, Hkv, page_size, Dv] (any strides, the last
+    dimension contiguous), page_table [B, max_pages]."""
+    if not k_pages.is_cuda:
+        raise ValueError("every tensor must be a device tensor")
+    if k_pages.dim() != 4 or v_pages.dim() != 4 or k_pages.shape[:3] != v_pages.shape[:3] or page_table.dim() != 2:
+        raise ValueError(f"shape mismatch: k_pages{tuple(k_pages.shape)} v_pages{tuple(v_pages.shape)} page_table{tuple(page_table.shape)}")
+    dev, dt = k_pages.device, _storage_dtype(k_pages)
+    _need_rows(dev, k_pages.dtype, ("k_pages", k_pages), ("v_pages", v_pages))
+    _need_int32(dev, ("page_table", page_table, None))
+    n, H, ps, Dk = k_pages.shape
+    return CacheDesc(page_table.shape[0], H, Dk, v_pages.shape[3], ps, n, page_table.shape[1], dt,
+                     *(_stride(k_pages, i) for i in range(3)), *(_stride(v_pages, i) for i in range(3)))
+
+
+class Attention(NamedTuple):
+    out: torch.Tensor                       # [B, Hq, Dv], in the cache's type
+    lse: Optional[torch.Tensor] = None      # [B, Hq] float32: ln of the sum of the exponentials of the scores
+
+
+def prepare_attend(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
+                   lengths: torch.Tensor, *, scale: Optional[float] = None, starts: Optional[torch.Tensor] = None,
+                   max_len: Optional[int] = None, mass: Optional[torch.Tensor] = None, want_lse: bool = False,
+                   out: Optional[Attention] = None, workspace: Optional[torch.Tensor] = None) -> Prepared:
+    """Check and marshal one attend call; the returned object runs it (see `attend` for the arguments)."""
+    c = _cache_desc(k_pages, v_pages, page_table)
+    dev, B = k_pages.device, c.B
+    if q.dim() != 3 or q.shape[0] != B or q.shape[2] != c.Dk:
+        raise ValueError(f"q must be [{B}, heads, {c.Dk}]")
+    Hq = q.shape[1]
+    _need_rows(dev, k_pages.dtype, ("q", q))
+    _need_int32(dev, ("lengths", lengths, (B,)), ("starts", starts, (B,)))
+    if max_len is None:
+        max_len = c.max_pages * c.page_size
+    if mass is not None:
+        _need_mass(dev, "mass", mass, B, c.Hkv, max_len)
+    if out is None:
+        out = Attention(torch.empty((B, Hq, c.Dv), dtype=q.dtype, device=dev),
+                        torch.empty((B, Hq), dtype=torch.float32, device=dev) if want_lse else None)
+    else:
+        _need_device(out.out, out.lse)
+        if tuple(out.out.shape) != (B, Hq, c.Dv) or out.out.dtype != q.dtype or \
+                (out.lse is not None and (tuple(out.lse.shape) != (B, Hq) or out.lse.dtype != torch.float32)):
+            raise ValueError("out buffers have the wrong shape or dtype")
+    a = AttendDesc(Hq, max_len, c.Dk ** -0.5 if scale is None else scale, 0, _stride(q, 0), _stride(q, 1),
+                   0 if mass is None else mass.shape[2])
+    need = lib().paep_attend_workspace_bytes(ctypes.byref(c), ctypes.byref(a), int(mass is not None))
+    if workspace is None and need > 0:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    args = (ctypes.byref(c), ctypes.byref(a), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(lengths),
+            _ptr(starts), _ptr(out.out), _ptr(out.lse), _ptr(mass), _ptr(workspace), ws_bytes)
+    return Prepared(lib().paep_attend, "paep_attend", args,
+                    (c, a, q, k_pages, v_pages, page_table, lengths, starts, mass, workspace), out)
+
+
+def attend(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *,
+           scale: Optional[float] = None, starts: Optional[torch.Tensor] = None, max_len: Optional[int] = None,
+           mass: Optional[torch.Tensor] = None, want_lse: bool = False, out: Optional[Attention] = None,
+           workspace: Optional[torch.Tensor] = None, stream=None) -> Attention:
+    """Attention of one new token per sequence over a paged key-value cache.
+
+    q [B, Hq, Dk] (any strides, the last dimension contiguous; so the pools), k_pages [n_pages, Hkv, page_size, Dk],
+    v_pages [n_pages, Hkv, page_size, Dv], page_table [B, max_pages] int32, lengths [B] int32 -> out [B, Hq, Dv],
+    lse [B, Hq] with want_lse.  A page that holds its slots outside its heads is passed as its transposed view.
+    `scale` defaults to Dk ** -0.5; `starts` [B] int32: the first position each sequence looks at; `max_len`: a bound on
+    the lengths (default: what a row of the page table can hold) -- the work is laid out for it, so a tight one is faster;
+    `mass` [B, Hkv, >= max_len] float32: increased by the attention weight of every position, summed over the query heads
+    of its key-value head (what `cache_evict` goes by).  Sequences with nothing to look at give zeros."""
+    with _on(stream):
+        prep = prepare_attend(q, k_pages, v_pages, page_table, lengths, scale=scale, starts=starts, max_len=max_len, mass=mass,
+                              want_lse=want_lse, out=out, workspace=workspace)
+    return prep(stream)
+
+
+def cache_append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
+                 positions: torch.Tensor, *, sequences: Optional[torch.Tensor] = None, mass: Optional[torch.Tensor] = None,
+                 stream=None) -> None:
+    """Write keys k [n, Hkv, Dk] and values v [n, Hkv, Dv] (rows any stride apart) into the cache: row i to position
+    positions[i] of sequence sequences[i] (default: of sequence i).  Rows that name no place are skipped.  `mass`
+    [B, Hkv, any] is set to 0 at the positions written."""
+    c = _cache_desc(k_pages, v_pages, page_table)
+    dev = k_pages.device
+    _need_rows(dev, k_pages.dtype, ("k", k), ("v", v))
+    n = k.shape[0]
+    if tuple(k.shape) != (n, c.Hkv, c.Dk) or tuple(v.shape) != (n, c.Hkv, c.Dv) or (c.Hkv > 1 and (k.stride(1) != c.Dk or v.stride(1) != c.Dv)):
+        raise ValueError(f"k must be [n, {c.Hkv}, {c.Dk}] and v [n, {c.Hkv}, {c.Dv}], the heads of a row side by side")
+    _need_int32(dev, ("positions", positions, (n,)), ("sequences", sequences, (n,)))
+    if mass is not None:
+        _need_mass(dev, "mass", mass, c.B, c.Hkv, 0)
+    st = lib().paep_cache_append(ctypes.byref(c), n, _ptr(k), _stride(k, 0), _ptr(v), _stride(v, 0), _ptr(k_pages), _ptr(v_pages),
+                                 _ptr(page_table), _ptr(sequences), _ptr(positions), _ptr(mass),
+                                 0 if mass is None else mass.shape[2], _stream_ptr(stream))
+    if st != 0:
+        raise PaepError(st, "paep_cache_append")
+
+
+class Eviction(NamedTuple):
+    lengths: torch.Tensor     # [B] int32: the lengths now
+    kept: torch.Tensor        # [B, Hkv, budget] int32: the positions kept, ascending, then -1
+    mass: torch.Tensor        # [B, Hkv, as before] float32: their accumulated weight, then 0
+
+
+def cache_evict(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor,
+                mass: torch.Tensor, out_table: torch.Tensor, budget: int, recent: int, *, max_len: Optional[int] = None,
+                out: Optional[Eviction] = None, stream=None) -> Eviction:
+    """Cut every sequence down to `budget` positions: each head keeps its last `recent` ones and, of those before them, the
+    ones with the largest accumulated weight `mass` [B, Hkv, >= max_len]; they are copied, in order, to the pages of
+    out_table [B, out_pages] int32 of the same pools, which must be free.  Shorter sequences are copied whole."""
+    c = _cache_desc(k_pages, v_pages, page_table)
+    dev, B, H = k_pages.device, c.B, c.Hkv
+    if max_len is None:
+        max_len = c.max_pages * c.page_size
+    _need_mass(dev, "mass", mass, B, H, max_len)
+    if out_table.dim() != 2 or out_table.shape[0] != B:
+        raise ValueError("out_table must be [B, out_pages]")
+    _need_int32(dev, ("lengths", lengths, (B,)), ("out_table", out_table, None))
+    if budget < 1:
+        raise ValueError("budget must be at least 1")
+    if out is None:
+        with _on(stream):
+            out = Eviction(torch.empty_like(lengths), torch.empty((B, H, budget), dtype=torch.int32, device=dev),
+                           torch.empty_like(mass))
+    else:
+        _need_int32(dev, ("out.lengths", out.lengths, (B,)), ("out.kept", out.kept, (B, H, budget)))
+        _need_mass(dev, "out.mass", out.mass, B, H, min(budget, max_len))
+        if out.mass.data_ptr() == mass.data_ptr() or out.lengths.data_ptr() == lengths.data_ptr():
+            raise ValueError("out.mass and out.lengths must be other buffers than mass and lengths")
+    st = lib().paep_cache_evict(ctypes.byref(c), max_len, budget, recent, _ptr(k_pages), _ptr(v_pages), _ptr(page_table),
+                                _ptr(lengths), _ptr(mass), mass.shape[2], _ptr(out_table), out_table.shape[1], _ptr(out.kept),
+                                _ptr(out.mass), out.mass.shape[2], _ptr(out.lengths), _stream_ptr(stream))
+    if st != 0:
+        raise PaepError(st, "paep_cache_evict")
+    return out
+
+
+class MoeOutput(NamedTuple):
+    y: torch.Tensor           # [T, d]
+    idx: torch.Tensor         # [T, k] int32
+    probs: torch.Tensor       # [T, k] float32
+
+
+def _prepare_moe(x, W13, W2, k, act, prob, residual, y, workspace):
+    """Shape and type checks shared by the expert-layer calls; returns the descriptor, y, the workspace and its size."""
+    if x.dim() != 2 or W13.dim() != 3 or W2.dim() != 3:
+        raise ValueError("x must be [T, d], W13 [E, 2f, d], W2 [E, d, f]")
+    T, d = x.shape
+    E, _, f = W2.shape
+    if tuple(W13.shape) != (E, 2 * f, d) or W2.shape[1] != d:
+        raise ValueError(f"shape mismatch: x{tuple(x.shape)} W13{tuple(W13.shape)} W2{tuple(W2.shape)}")
+    _need_device(x, W13, W2, residual, y)
+    dt = _storage_dtype(x)
+    for t in (W13, W2, residual, y):
+        if t is not None and (t.dtype != x.dtype or t.device != x.device):
+            raise TypeError("x, the weights, residual and y must share one storage dtype and device")
+    for t in (residual, y):
+        if t is not None and t.shape != x.shape:
+            raise ValueError("residual and y must be [T, d]")
+    desc = MoeDesc(T, d, f, E, k, dt, ACT[act], PROB[prob])
+    if y is None:
+        y = torch.empty_like(x)
+    need = lib().paep_moe_workspace_bytes(ctypes.byref(desc))
+    if workspace is None and need > 0:
+        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    return desc, y, workspace, 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def prepare_moe_layer(x: torch.Tensor, Wg: torch.Tensor, W13: torch.Tensor, W2: torch.Tensor, k: int, *,
+                      bg: Optional[torch.Tensor] = None, act: str = "silu", prob: str = "softmax",
+                      residual: Optional[torch.Tensor] = None, counts: Optional[torch.Tensor] = None,
+                      out: Optional[MoeOutput] = None, workspace: Optional[torch.Tensor] = None) -> Prepared:
+    """Check and marshal one moe_layer call; the returned object runs it (see `moe_layer` for the arguments)."""
+    desc, y, workspace, ws_bytes = _prepare_moe(x, W13, W2, k, act, prob, residual, None if out is None else out.y, workspace)
+    T, E, dev = desc.T, desc.E, x.device
+    _need_device(Wg, bg, counts)
+    if tuple(Wg.shape) != (E, desc.d) or Wg.dtype != x.dtype or Wg.device != dev:
+        raise ValueError("Wg must be [E, d] in the storage dtype and on the device of x")
+    if bg is not None and (bg.numel() != E or bg.dtype != x.dtype or bg.device != dev):
+        raise ValueError("bg must be [E] in the storage dtype and on the device of x")
+    if counts is not None and (counts.dtype != torch.int32 or counts.numel() != E or counts.device != dev):
+        raise ValueError("counts must be int32 [E]")
+    if out is None:
+        out = MoeOutput(y, torch.empty((T, k), dtype=torch.int32, device=dev), torch.empty((T, k), dtype=torch.float32, device=dev))
+    else:
+        _need_device(out.idx, out.probs)
+        if tuple(out.idx.shape) != (T, k) or out.idx.dtype != torch.int32 or tuple(out.probs.shape) != (T, k) \
+                or out.probs.dtype != torch.float32:
+            raise ValueError("out buffers have the wrong shape or dtype")
+    args = (ctypes.byref(desc), _ptr(x), _ptr(Wg), _ptr(bg), _ptr(W13), _ptr(W2), _ptr(residual), _ptr(out.y), _ptr(out.idx),
+            _ptr(out.probs), _ptr(counts), _ptr(workspace), ws_bytes)
+    return Prepared(lib().paep_moe_layer, "paep_moe_layer", args, (desc, x, Wg, bg, W13, W2, residual, counts, workspace), out)
+
+
+def moe_layer(x: torch.Tensor, Wg: torch.Tensor, W13: torch.Tensor, W2: torch.Tensor, k: int, *,
+              bg: Optional[torch.Tensor] = None, act: str = "silu", prob: str = "softmax",
+              residual: Optional[torch.Tensor] = None, counts: Optional[torch.Tensor] = None,
+              out: Optional[MoeOutput] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> MoeOutput:
+    """A mixture-of-experts layer for up to 64 tokens: x [T, d], router Wg [E, d] (+ bg [E]), W13 [E, 2f, d] (the f gate rows,
+    then the f others), W2 [E, d, f] -> y [T, d], idx [T, k], probs [T, k] with
+
+        y = residual + sum over the k experts of  p * W2 (act(W1 x) * (W3 x)).
+
+    `prob` says what weighs an expert, as in `predict`; `counts` (int32 [E]) is increased by the tokens per expert.
+    Weights and tokens bf16 or float32, sums in float32."""
+    with _on(stream):
+        prep = prepare_moe_layer(x, Wg, W13, W2, k, bg=bg, act=act, prob=prob, residual=residual, counts=counts, out=out,
+                                 workspace=workspace)
+    return prep(stream)
+
+
+def moe_experts(x: torch.Tensor, W13: torch.Tensor, W2: torch.Tensor, idx: torch.Tensor, probs: torch.Tensor, *,
+                act: str = "silu", residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """`moe_layer` with a selection that is there already, idx [T, k] int32 and probs [T, k] float32 (another router's, or
+    the predictor's own); ids outside [0, E) are skipped.  Returns y [T, d]."""
+    if idx.dim() != 2 or idx.shape != probs.shape or idx.shape[0] != x.shape[0] or idx.dtype != torch.int32 \
+            or probs.dtype != torch.float32 or idx.device != x.device or probs.device != x.device:
+        raise ValueError("idx must be int32 [T, k] and probs float32 [T, k], on the device of x")
+    _need_device(idx, probs)
+    with _on(stream):
+        desc, y, workspace, ws_bytes = _prepare_moe(x, W13, W2, idx.shape[1], act, "softmax", residual, out, workspace)
+    st = lib().paep_moe_experts(ctypes.byref(desc), _ptr(x), _ptr(W13), _ptr(W2), _ptr(idx), _ptr(probs), _ptr(residual), _ptr(y),
+                                _ptr(workspace), ws_bytes, _stream_ptr(stream))
+    if st != 0:
+        raise PaepError(st, "paep_moe_experts")
+    return y
 
 
 def probe_read(src: torch.Tensor, sink: torch.Tensor, stream=None) -> None:

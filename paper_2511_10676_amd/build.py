@@ -18,7 +18,8 @@ LIB = os.path.join(HERE, "libpaep.so")
 
 SOURCES = ["paep_api.cpp", "predict_simple.hip", "predict_f32.hip", "finalize.hip",
            "predict_decode.hip", "predict_prefill.hip", "prefill256.hip",
-           "group.hip", "score.hip", "profile.hip", "probe.hip", "fold.hip"]
+           "group.hip", "score.hip", "profile.hip", "probe.hip", "fold.hip",
+           "decode_step_api.cpp", "attend.hip", "cache.hip", "moe.hip"]
 
 # The target feature switches the packed fp32 vector instructions (v_pk_add_f32, v_pk_mul_f32,
 # v_pk_fma_f32) off in every device compile.  hipcc's host pass does not know the feature and says so

@@ -93,7 +93,7 @@ int resolve(const paep_predict_desc* d, const paep::PredictArgs& a)
 
 extern "C" {
 
-int paep_version(void) { return 100; }
+int paep_version(void) { return 200; }
 
 const char* paep_status_string(paep_status s)
 {

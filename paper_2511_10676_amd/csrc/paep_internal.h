@@ -102,4 +102,61 @@ hipError_t launch_confidence_select(const int32_t* idx, const float* probs, int 
                                     float ratio, int32_t* idx_out, int32_t* k_row, int32_t* n_wide,
                                     hipStream_t stream);
 
+
+// ---- paged key-value cache, attention of one new token, expert layer ----
+
+// A cache as the kernels see it: strides in bytes, page_size = 1 << page_shift.
+struct CacheView {
+    int B, Hkv, Dk, Dv, page_shift, n_pages, max_pages, dtype;
+    long long k_page, k_head, k_slot, v_page, v_head, v_slot;
+    const int32_t* table;
+    unsigned char* k;
+    unsigned char* v;
+};
+
+struct AttendArgs {
+    CacheView c;
+    int Hq, max_len;
+    float scale;
+    long long q_seq, q_head;       // bytes
+    const void* q;
+    const int32_t* lengths;
+    const int32_t* starts;         // nullable
+    void* out;
+    float* lse;                    // nullable
+    float* mass;                   // nullable
+    long long mass_stride;         // floats
+    void* workspace;
+    hipStream_t stream;
+};
+bool attend_fits(const AttendArgs& a);                       // the grid holds this shape
+size_t attend_workspace_bytes(const AttendArgs& a);          // (a.mass: whether there is one)
+hipError_t launch_attend(const AttendArgs& a);
+
+hipError_t launch_cache_append(const CacheView& c, int n, const void* k, long long k_row, const void* v, long long v_row,
+                               const int32_t* sequences, const int32_t* positions, float* mass, long long mass_stride,
+                               hipStream_t stream);
+hipError_t launch_cache_evict(const CacheView& c, int max_len, int budget, int recent, const int32_t* lengths,
+                              const float* mass, long long mass_stride, const int32_t* out_table, int out_max_pages,
+                              int32_t* kept, float* mass_out, long long mass_out_stride, int32_t* lengths_out,
+                              hipStream_t stream);
+
+struct MoeArgs {
+    int T, d, f, E, k, dtype, act, prob_mode;
+    const void* x;
+    const void* Wg;                // null: idx and probs are inputs
+    const void* bg;                // nullable
+    const void* W13;
+    const void* W2;
+    const void* residual;          // nullable
+    void* y;
+    int32_t* idx;
+    float* probs;
+    int32_t* counts;               // nullable
+    void* workspace;
+    hipStream_t stream;
+};
+size_t moe_workspace_bytes(const MoeArgs& a);
+hipError_t launch_moe(const MoeArgs& a);
+
 }  // namespace paep
