@@ -189,6 +189,8 @@ def test_attend_strided_queries_given_buffers_streams_and_repeats(dtype):
         B.attend(*args, mass=torch.zeros((3, 2, 9), device="cuda"))
     with pytest.raises(B.PaepError, match="PAEP_ERR_SHAPE"):
         B.attend(args[0][:, :3], *args[1:])
+    with pytest.raises(B.PaepError, match="PAEP_ERR_WORKSPACE"):
+        B.attend(args[0], *args[1:], mass=torch.zeros((3, 2, 1200), device="cuda"), max_len=1200, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
 
 
 def test_attend_is_the_same_every_time_and_empty_batches_are_fine():
