@@ -476,8 +476,8 @@ paep_status paep_cache_evict(const paep_cache_desc *cache, int32_t max_len, int3
 /* Shape of a mixture-of-experts layer for a few tokens. */
 typedef struct {
     int32_t T;          /* tokens, 0..PAEP_MOE_MAX_T */
-    int32_t d;          /* hidden size, multiple of 8, >= 8 */
-    int32_t f;          /* inner width of an expert, multiple of 8, >= 8 */
+    int32_t d;          /* hidden size, multiple of 8, 8..65536 */
+    int32_t f;          /* inner width of an expert, multiple of 8, 8..65536 */
     int32_t E;          /* experts, 1..PAEP_MAX_E */
     int32_t k;          /* experts per token, 1..min(E, PAEP_MAX_K) */
     int32_t dtype;      /* paep_dtype of x, the weights, residual and y */

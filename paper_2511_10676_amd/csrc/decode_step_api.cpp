@@ -95,7 +95,7 @@ paep_status check_moe(const paep_moe_desc* d)
     if (d->prob != PAEP_PROB_SOFTMAX_ALL && d->prob != PAEP_PROB_SOFTMAX_TOPK && d->prob != PAEP_PROB_SIGMOID)
         return PAEP_ERR_DTYPE;
     if (d->T < 0 || d->T > PAEP_MOE_MAX_T || d->E < 1 || d->E > PAEP_MAX_E) return PAEP_ERR_SHAPE;
-    if (d->d < 8 || d->d % 8 || d->d > (1 << 20) || d->f < 8 || d->f % 8 || d->f > (1 << 20)) return PAEP_ERR_SHAPE;
+    if (d->d < 8 || d->d % 8 || d->d > 65536 || d->f < 8 || d->f % 8 || d->f > 65536) return PAEP_ERR_SHAPE;
     if (d->k < 1 || d->k > d->E || d->k > PAEP_MAX_K) return PAEP_ERR_K;
     return PAEP_OK;
 }
