@@ -55,16 +55,21 @@ hipError_t launch_cache_append(const CacheView& c, int n, const void* k, long lo
 // Eviction.  Kernel 1: which positions each head keeps; kernel 2: their rows are copied.
 // ---------------------------------------------------------------------------
 static constexpr int SEL_THREADS = 1024, SEL_WAVES = SEL_THREADS / 64;
+static constexpr int SEL_KEYS = 32;                  // masses of a thread at a time
+static constexpr int SEL_SPAN = SEL_THREADS * SEL_KEYS;
+static constexpr int SEL_COPIES = 8;                 // of every counter, a lane's by its number: most masses share a few digits
 
 // A workgroup per sequence and head.  The (budget - recent)-th largest mass is found digit by digit on the ordered 32-bit
-// patterns (four histograms of 8 bits in LDS); everything above it is kept, and of its equals the lowest positions.
+// patterns (four histograms of 8 bits in LDS); everything above it is kept, and of its equals the lowest positions.  Up to
+// SEL_SPAN masses stay in registers from the first histogram to the last store; longer sequences are read again for each.
 __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(
     int Hkv, int max_len, int budget, int recent, const int32_t* __restrict__ lengths, const float* __restrict__ mass,
     long long mass_stride, int32_t* __restrict__ kept, float* __restrict__ mass_out, long long mass_out_stride,
     int32_t* __restrict__ lengths_out)
 {
-    __shared__ uint32_t hist[256], chosen[2];
-    __shared__ uint32_t totals[SEL_WAVES];
+    __shared__ uint32_t hist[256][SEL_COPIES], chosen[2];
+    __shared__ uint32_t counts[SEL_KEYS * SEL_WAVES];        // of a span, per 64 positions: above the threshold | at it << 16; then what is before
+    __shared__ uint32_t carry[2];
     const int b = blockIdx.x / Hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = clamped_length(lengths, b, max_len);
     const float* in = mass + (long long)blockIdx.x * mass_stride;
@@ -82,24 +87,53 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(
     for (int j = tid; j < recent; j += SEL_THREADS) { ids[best + j] = old + j; out[best + j] = in[old + j]; }
     if (best == 0) return;
 
+    uint32_t key[SEL_KEYS];                                  // of position p0 + u * SEL_THREADS + tid; 0, below every number's, where there is none
+    auto load = [&](long long p0) {
+        float m[SEL_KEYS];
+#pragma unroll
+        for (int u = 0; u < SEL_KEYS; ++u) {
+            const long long p = p0 + u * SEL_THREADS + tid;
+            m[u] = in[p < old ? p : 0];
+        }
+#pragma unroll
+        for (int u = 0; u < SEL_KEYS; ++u) key[u] = orderable(m[u]);
+    };
+    const bool whole = old <= SEL_SPAN;
+    if (whole) load(0);
+
     uint32_t threshold = 0, need = best;                     // the threshold's digits so far, and its rank among the keys that share them
     for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) hist[tid] = 0;
+        for (int i = tid; i < 256 * SEL_COPIES; i += SEL_THREADS) (&hist[0][0])[i] = 0;
         __syncthreads();
-        for (int p = tid; p < old; p += SEL_THREADS) {
-            const uint32_t key = orderable(in[p]);
-            if (shift == 24 || (key >> (shift + 8)) == (threshold >> (shift + 8))) atomicAdd(&hist[(key >> shift) & 255u], 1u);
+        for (long long p0 = 0; p0 < old; p0 += SEL_SPAN) {
+            if (!whole) load(p0);
+            const uint32_t within = shift == 24 ? 0xFFFFFFFFu : (1u << (shift + 8)) - 1u;      // keys that share the threshold's digits
+#pragma unroll
+            for (int u = 0; u < SEL_KEYS; ++u) {
+                if (p0 + u * SEL_THREADS >= old) break;
+                if ((key[u] ^ threshold) <= within && p0 + u * SEL_THREADS + tid < old)
+                    atomicAdd(&hist[(key[u] >> shift) & 255u][lane % SEL_COPIES], 1u);
+            }
+        }
+        __syncthreads();
+        if (tid < 256) {                                     // (a row's copies in an order that spreads over the banks)
+            uint32_t c = 0;
+#pragma unroll
+            for (int i = 0; i < SEL_COPIES; ++i) c += hist[tid][(i + tid) % SEL_COPIES];
+            counts[tid] = c;
         }
         __syncthreads();
         if (wave == 0) {                                     // lane l: digits 255 - 4l .. 252 - 4l
             uint32_t c[4], sum = 0;
-            for (int u = 0; u < 4; ++u) { c[u] = hist[255 - 4 * lane - u]; sum += c[u]; }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) { c[u] = counts[255 - 4 * lane - u]; sum += c[u]; }
             uint32_t upto = sum;                             // inclusive over lanes
             for (int s = 1; s < 64; s <<= 1) {
                 const uint32_t o = __shfl_up(upto, s, 64);
                 if (lane >= s) upto += o;
             }
             uint32_t before = upto - sum;
+#pragma unroll
             for (int u = 0; u < 4; ++u) {
                 if (before < need && need <= before + c[u]) { chosen[0] = 255 - 4 * lane - u; chosen[1] = need - before; }
                 before += c[u];
@@ -111,56 +145,102 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(
         __syncthreads();
     }
     // in ascending position: everything above the threshold and the first `need` at it
-    uint32_t above = 0, equal = 0;                           // of the positions before this tile
-    for (int p0 = 0; p0 < old; p0 += SEL_THREADS) {
-        const int p = p0 + tid;
-        const float m = p < old ? in[p] : 0.0f;
-        const uint32_t key = orderable(m);
-        const bool gt = p < old && key > threshold, eq = p < old && key == threshold;
-        const unsigned long long bg = __ballot(gt), be = __ballot(eq), lower = (1ull << lane) - 1;
-        if (lane == 0) totals[wave] = (uint32_t)__popcll(bg) | (uint32_t)__popcll(be) << 16;
-        __syncthreads();
-        uint32_t g = above + (uint32_t)__popcll(bg & lower), e = equal + (uint32_t)__popcll(be & lower);
-        for (int w = 0; w < SEL_WAVES; ++w) {
-            const uint32_t t = totals[w];
-            if (w < wave) { g += t & 0xFFFFu; e += t >> 16; }
-            above += t & 0xFFFFu;
-            equal += t >> 16;
-        }
-        if (gt || (eq && e < need)) {
-            const uint32_t j = g + (e < need ? e : need);
-            ids[j] = p;
-            out[j] = m;
+    if (tid == 0) carry[0] = carry[1] = 0;
+    for (long long p0 = 0; p0 < old; p0 += SEL_SPAN) {
+        if (!whole) load(p0);
+#pragma unroll
+        for (int u = 0; u < SEL_KEYS; ++u) {
+            const bool there = p0 + u * SEL_THREADS + tid < old;
+            const uint32_t both = (uint32_t)__popcll(__ballot(there && key[u] > threshold)) |
+                                  (uint32_t)__popcll(__ballot(there && key[u] == threshold)) << 16;
+            if (lane == 0) counts[u * SEL_WAVES + wave] = both;
         }
         __syncthreads();
+        if (wave == 0) {                                     // what is before each 64 positions: lane l has 8 of them
+            constexpr int MINE = SEL_KEYS * SEL_WAVES / 64;
+            uint32_t c[MINE], sg = 0, se = 0;
+#pragma unroll
+            for (int i = 0; i < MINE; ++i) { c[i] = counts[lane * MINE + i]; sg += c[i] & 0xFFFFu; se += c[i] >> 16; }
+            uint32_t ug = sg, ue = se;
+            for (int s = 1; s < 64; s <<= 1) {
+                const uint32_t og = __shfl_up(ug, s, 64), oe = __shfl_up(ue, s, 64);
+                if (lane >= s) { ug += og; ue += oe; }
+            }
+            uint32_t g = ug - sg, e = ue - se;               // (up to 32768 each: 16 bits)
+#pragma unroll
+            for (int i = 0; i < MINE; ++i) {
+                counts[lane * MINE + i] = g | e << 16;
+                g += c[i] & 0xFFFFu;
+                e += c[i] >> 16;
+            }
+        }
+        __syncthreads();
+        const uint32_t g0 = carry[0], e0 = carry[1];
+        uint32_t ng = 0, ne = 0;
+#pragma unroll
+        for (int u = 0; u < SEL_KEYS; ++u) {
+            if (p0 + u * SEL_THREADS >= old) break;
+            const long long p = p0 + u * SEL_THREADS + tid;
+            const bool g = p < old && key[u] > threshold, e = p < old && key[u] == threshold;
+            const unsigned long long bg = __ballot(g), be = __ballot(e);
+            const uint32_t c = counts[u * SEL_WAVES + wave];
+            ng = g0 + (c & 0xFFFFu) + __builtin_amdgcn_mbcnt_hi((uint32_t)(bg >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)bg, 0));
+            ne = e0 + (c >> 16) + __builtin_amdgcn_mbcnt_hi((uint32_t)(be >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)be, 0));
+            if (g || (e && ne < need)) {
+                const uint32_t j = ng + min(ne, need);
+                ids[j] = (int32_t)p;
+                out[j] = in[p];
+            }
+            ng += g ? 1u : 0u;
+            ne += e ? 1u : 0u;
+        }
+        __syncthreads();
+        if (tid == SEL_THREADS - 1) {                        // (a further span follows a full one only)
+            carry[0] = ng;
+            carry[1] = ne;
+        }
     }
 }
 
-static constexpr int MOVE_THREADS = 256, MOVE_ROWS = 64;
+static constexpr int MOVE_THREADS = 256, MOVE_ROWS = 64, MOVE_PIECES = 8;
 
-// A workgroup per sequence, head and MOVE_ROWS kept positions: 16-byte pieces of their keys and values.
+// A workgroup per sequence, head and MOVE_ROWS kept positions.  Where a row comes from and goes to is looked up once, by one
+// thread; then every thread copies 16-byte pieces of keys and values, MOVE_PIECES of them requested together.
 __global__ __launch_bounds__(MOVE_THREADS) void evict_move_kernel(CacheView c, int k_pieces, int v_pieces, int budget, int parts,
                                                                   const int32_t* __restrict__ kept,
                                                                   const int32_t* __restrict__ out_table, int out_max_pages)
 {
+    __shared__ long long k_from[MOVE_ROWS], k_to[MOVE_ROWS], v_from[MOVE_ROWS], v_to[MOVE_ROWS];      // k_from < 0: nothing to copy
     const int row = blockIdx.x / parts, part = blockIdx.x % parts;
     const int b = row / c.Hkv, h = row % c.Hkv, slots = (1 << c.page_shift) - 1;
-    const int32_t* ids = kept + (long long)row * budget;
+    bool any = false;
+    if (threadIdx.x < MOVE_ROWS) {
+        const int i = threadIdx.x, j = part * MOVE_ROWS + i;
+        const int p = j < budget ? kept[(long long)row * budget + j] : -1;
+        const int from = p < 0 ? -1 : page_entry(c.table, c.max_pages, c.n_pages, b, p >> c.page_shift);
+        const int to = p < 0 ? -1 : page_entry(out_table, out_max_pages, c.n_pages, b, j >> c.page_shift);
+        any = from >= 0 && to >= 0;
+        k_from[i] = any ? from * c.k_page + h * c.k_head + (p & slots) * c.k_slot : -1;
+        k_to[i] = any ? to * c.k_page + h * c.k_head + (j & slots) * c.k_slot : 0;
+        v_from[i] = any ? from * c.v_page + h * c.v_head + (p & slots) * c.v_slot : 0;
+        v_to[i] = any ? to * c.v_page + h * c.v_head + (j & slots) * c.v_slot : 0;
+    }
+    if (!__syncthreads_or(any)) return;
     const int per = k_pieces + v_pieces;
-    for (int i = threadIdx.x; i < MOVE_ROWS * per; i += MOVE_THREADS) {
-        const int j = part * MOVE_ROWS + i / per, piece = i % per;
-        if (j >= budget) break;
-        const int p = ids[j];
-        if (p < 0) continue;
-        const int from = page_entry(c.table, c.max_pages, c.n_pages, b, p >> c.page_shift);
-        const int to = page_entry(out_table, out_max_pages, c.n_pages, b, j >> c.page_shift);
-        if (from < 0 || to < 0) continue;
-        if (piece < k_pieces)
-            *(u32x4*)(c.k + to * c.k_page + h * c.k_head + (j & slots) * c.k_slot + piece * 16) =
-                *(const u32x4*)(c.k + from * c.k_page + h * c.k_head + (p & slots) * c.k_slot + piece * 16);
-        else
-            *(u32x4*)(c.v + to * c.v_page + h * c.v_head + (j & slots) * c.v_slot + (piece - k_pieces) * 16) =
-                *(const u32x4*)(c.v + from * c.v_page + h * c.v_head + (p & slots) * c.v_slot + (piece - k_pieces) * 16);
+    for (int i0 = threadIdx.x; i0 < MOVE_ROWS * per; i0 += MOVE_PIECES * MOVE_THREADS) {
+        u32x4 f[MOVE_PIECES];
+        unsigned char* to[MOVE_PIECES];
+#pragma unroll
+        for (int u = 0; u < MOVE_PIECES; ++u) {
+            const int i = min(i0 + u * MOVE_THREADS, MOVE_ROWS * per - 1), r = i / per, q = i - r * per;
+            const bool is_k = q < k_pieces, there = i0 + u * MOVE_THREADS < MOVE_ROWS * per && k_from[r] >= 0;
+            const int off = (is_k ? q : q - k_pieces) * 16;
+            to[u] = !there ? nullptr : is_k ? c.k + k_to[r] + off : c.v + v_to[r] + off;
+            f[u] = *(const u32x4*)(!there ? c.k : is_k ? c.k + k_from[r] + off : c.v + v_from[r] + off);
+        }
+#pragma unroll
+        for (int u = 0; u < MOVE_PIECES; ++u)
+            if (to[u]) *(u32x4*)to[u] = f[u];
     }
 }
 
