@@ -11,6 +11,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
+import struct
 from typing import NamedTuple, Optional
 
 import torch
@@ -57,6 +58,10 @@ class CacheDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hkv", "Dk", "Dv", "page_size", "n_pages", "max_pages", "dtype")] + \
                [(n, ctypes.c_int64) for n in ("k_page_stride", "k_head_stride", "k_slot_stride",
                                               "v_page_stride", "v_head_stride", "v_slot_stride")]
+
+
+# the same bytes as the two structures, in a third of the time
+_CACHE_BYTES, _ATTEND_BYTES = struct.Struct("8i6q"), struct.Struct("2ifi3q")
 
 
 class AttendDesc(ctypes.Structure):
@@ -131,7 +136,7 @@ def lib() -> ctypes.CDLL:
         L.paep_probe_read.restype = ctypes.c_int
         L.paep_probe_mfma.argtypes = [i32, i32, vp, sz, vp, ctypes.POINTER(ctypes.c_double)]
         L.paep_probe_mfma.restype = ctypes.c_int
-        i64, cp, ap, mp = ctypes.c_int64, ctypes.POINTER(CacheDesc), ctypes.POINTER(AttendDesc), ctypes.POINTER(MoeDesc)
+        i64, cp, ap, mp = ctypes.c_int64, vp, vp, ctypes.POINTER(MoeDesc)      # (cp, ap: the structure by reference, or its bytes)
         L.paep_attend_workspace_bytes.argtypes = [cp, ap, i32]
         L.paep_attend_workspace_bytes.restype = sz
         L.paep_attend.argtypes = [cp, ap] + [vp] * 10 + [sz, vp]
@@ -154,13 +159,15 @@ def lib() -> ctypes.CDLL:
 
 
 def _ptr(t: Optional[torch.Tensor]):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
-def _stream_ptr(stream) -> ctypes.c_void_p:
+def _stream_ptr(stream) -> int:
     if stream is None:
-        stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream)
+        # torch.cuda.current_stream() makes a Stream object: 3 us, as long as the shortest kernels here
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
+    return stream.cuda_stream
 
 
 def _on(stream):
@@ -552,24 +559,20 @@ def fold_batchnorm(W1: torch.Tensor, b1: Optional[torch.Tensor], gamma: torch.Te
 
 # ---- a layer's decode step beside the predictor ----
 
-def _need_int32(dev, *named):
-    """Contiguous int32 tensors of the given shapes on `dev` (shape None: any; tensor None: left out)."""
-    for name, t, shape in named:
-        if t is None:
-            continue
-        if t.dtype != torch.int32 or t.device != dev or not t.is_contiguous() or (shape is not None and tuple(t.shape) != shape):
-            raise ValueError(f"{name} must be contiguous int32" + (f" {list(shape)}" if shape is not None else "") + " on the cache's device")
+def _need_int32(dev: int, name: str, t: torch.Tensor, shape) -> None:
+    """A contiguous int32 tensor on device `dev` (shape None: any)."""
+    if t.dtype is not torch.int32 or t.get_device() != dev or not t.is_contiguous() or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name} must be contiguous int32" + (f" {list(shape)}" if shape is not None else "") + " on the cache's device")
 
 
-def _need_rows(dev, dtype, *named):
-    """Tensors of the cache's type and device whose last dimension is contiguous."""
-    for name, t in named:
-        if t.dtype != dtype or t.device != dev or t.stride(-1) != 1:
-            raise ValueError(f"{name} must be of the cache's type and device, its last dimension contiguous")
+def _need_rows(dev: int, dtype, name: str, t: torch.Tensor) -> None:
+    """A tensor of the cache's type and device whose last dimension is contiguous."""
+    if t.dtype is not dtype or t.get_device() != dev or t.stride(-1) != 1:
+        raise ValueError(f"{name} must be of the cache's type and device, its last dimension contiguous")
 
 
-def _need_mass(dev, name, t, B, Hkv, least):
-    if t.dtype != torch.float32 or t.device != dev or not t.is_contiguous() or t.dim() != 3 or t.shape[0] != B \
+def _need_mass(dev: int, name: str, t: torch.Tensor, B: int, Hkv: int, least: int) -> None:
+    if t.dtype is not torch.float32 or t.get_device() != dev or not t.is_contiguous() or t.dim() != 3 or t.shape[0] != B \
             or t.shape[1] != Hkv or t.shape[2] < least:
         raise ValueError(f"{name} must be contiguous float32 [{B}, {Hkv}, at least {least}] on the cache's device")
 
@@ -579,19 +582,39 @@ def _stride(t: torch.Tensor, dim: int) -> int:
     return t.stride(dim) if t.shape[dim] > 1 else 0
 
 
-def _cache_desc(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor) -> CacheDesc:
+class _Cache(NamedTuple):
+    desc: bytes               # the paep_cache_desc
+    dev: int
+    B: int
+    Hkv: int
+    Dk: int
+    Dv: int
+    capacity: int             # positions of a page-table row
+
+
+def _cache(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor) -> _Cache:
     """The cache k_pages [n_pages, Hkv, page_size, Dk], v_pages [n_pages, Hkv, page_size, Dv] (any strides, the last
     dimension contiguous), page_table [B, max_pages]."""
-    if not k_pages.is_cuda:
+    dev, dtype = k_pages.get_device(), k_pages.dtype
+    if dev < 0 or not k_pages.is_cuda:
         raise ValueError("every tensor must be a device tensor")
+    dt = _storage_dtype(k_pages)
     if k_pages.dim() != 4 or v_pages.dim() != 4 or k_pages.shape[:3] != v_pages.shape[:3] or page_table.dim() != 2:
         raise ValueError(f"shape mismatch: k_pages{tuple(k_pages.shape)} v_pages{tuple(v_pages.shape)} page_table{tuple(page_table.shape)}")
-    dev, dt = k_pages.device, _storage_dtype(k_pages)
-    _need_rows(dev, k_pages.dtype, ("k_pages", k_pages), ("v_pages", v_pages))
-    _need_int32(dev, ("page_table", page_table, None))
     n, H, ps, Dk = k_pages.shape
-    return CacheDesc(page_table.shape[0], H, Dk, v_pages.shape[3], ps, n, page_table.shape[1], dt,
-                     *(_stride(k_pages, i) for i in range(3)), *(_stride(v_pages, i) for i in range(3)))
+    (kp, kh, ks, k1), (vp, vh, vs, v1) = k_pages.stride(), v_pages.stride()
+    if k1 != 1 or v1 != 1 or v_pages.dtype is not dtype or v_pages.get_device() != dev:
+        raise ValueError("k_pages and v_pages must be of one type and device, their last dimensions contiguous")
+    _need_int32(dev, "page_table", page_table, None)
+    B, width = page_table.shape
+    if n < 2:                                                # (see _stride)
+        kp = vp = 0
+    if H < 2:
+        kh = vh = 0
+    if ps < 2:
+        ks = vs = 0
+    Dv = v_pages.shape[3]
+    return _Cache(_CACHE_BYTES.pack(B, H, Dk, Dv, ps, n, width, dt, kp, kh, ks, vp, vh, vs), dev, B, H, Dk, Dv, width * ps)
 
 
 class Attention(NamedTuple):
@@ -604,35 +627,37 @@ def prepare_attend(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor
                    max_len: Optional[int] = None, mass: Optional[torch.Tensor] = None, want_lse: bool = False,
                    out: Optional[Attention] = None, workspace: Optional[torch.Tensor] = None) -> Prepared:
     """Check and marshal one attend call; the returned object runs it (see `attend` for the arguments)."""
-    c = _cache_desc(k_pages, v_pages, page_table)
-    dev, B = k_pages.device, c.B
+    c = _cache(k_pages, v_pages, page_table)
+    dev, B, dtype = c.dev, c.B, k_pages.dtype
     if q.dim() != 3 or q.shape[0] != B or q.shape[2] != c.Dk:
         raise ValueError(f"q must be [{B}, heads, {c.Dk}]")
     Hq = q.shape[1]
-    _need_rows(dev, k_pages.dtype, ("q", q))
-    _need_int32(dev, ("lengths", lengths, (B,)), ("starts", starts, (B,)))
+    _need_rows(dev, dtype, "q", q)
+    _need_int32(dev, "lengths", lengths, (B,))
+    if starts is not None:
+        _need_int32(dev, "starts", starts, (B,))
     if max_len is None:
-        max_len = c.max_pages * c.page_size
+        max_len = c.capacity
     if mass is not None:
         _need_mass(dev, "mass", mass, B, c.Hkv, max_len)
     if out is None:
-        out = Attention(torch.empty((B, Hq, c.Dv), dtype=q.dtype, device=dev),
-                        torch.empty((B, Hq), dtype=torch.float32, device=dev) if want_lse else None)
+        out = Attention(q.new_empty((B, Hq, c.Dv)), q.new_empty((B, Hq), dtype=torch.float32) if want_lse else None)
     else:
         _need_device(out.out, out.lse)
-        if tuple(out.out.shape) != (B, Hq, c.Dv) or out.out.dtype != q.dtype or \
+        if tuple(out.out.shape) != (B, Hq, c.Dv) or out.out.dtype != dtype or \
                 (out.lse is not None and (tuple(out.lse.shape) != (B, Hq) or out.lse.dtype != torch.float32)):
             raise ValueError("out buffers have the wrong shape or dtype")
-    a = AttendDesc(Hq, max_len, c.Dk ** -0.5 if scale is None else scale, 0, _stride(q, 0), _stride(q, 1),
-                   0 if mass is None else mass.shape[2])
-    need = lib().paep_attend_workspace_bytes(ctypes.byref(c), ctypes.byref(a), int(mass is not None))
+    d = _ATTEND_BYTES.pack(Hq, max_len, c.Dk ** -0.5 if scale is None else scale, 0, _stride(q, 0), _stride(q, 1),
+                           0 if mass is None else mass.shape[2])
+    L = lib()
+    need = L.paep_attend_workspace_bytes(c.desc, d, mass is not None)
     if workspace is None and need > 0:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        workspace = q.new_empty(need, dtype=torch.uint8)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    args = (ctypes.byref(c), ctypes.byref(a), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(lengths),
+    args = (c.desc, d, _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(lengths),
             _ptr(starts), _ptr(out.out), _ptr(out.lse), _ptr(mass), _ptr(workspace), ws_bytes)
-    return Prepared(lib().paep_attend, "paep_attend", args,
-                    (c, a, q, k_pages, v_pages, page_table, lengths, starts, mass, workspace), out)
+    return Prepared(L.paep_attend, "paep_attend", args,
+                    (q, k_pages, v_pages, page_table, lengths, starts, mass, workspace), out)
 
 
 def attend(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *,
@@ -660,16 +685,19 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_page
     """Write keys k [n, Hkv, Dk] and values v [n, Hkv, Dv] (rows any stride apart) into the cache: row i to position
     positions[i] of sequence sequences[i] (default: of sequence i).  Rows that name no place are skipped.  `mass`
     [B, Hkv, any] is set to 0 at the positions written."""
-    c = _cache_desc(k_pages, v_pages, page_table)
-    dev = k_pages.device
-    _need_rows(dev, k_pages.dtype, ("k", k), ("v", v))
+    c = _cache(k_pages, v_pages, page_table)
+    dev = c.dev
+    _need_rows(dev, k_pages.dtype, "k", k)
+    _need_rows(dev, k_pages.dtype, "v", v)
     n = k.shape[0]
-    if tuple(k.shape) != (n, c.Hkv, c.Dk) or tuple(v.shape) != (n, c.Hkv, c.Dv) or (c.Hkv > 1 and (k.stride(1) != c.Dk or v.stride(1) != c.Dv)):
+    if k.shape != (n, c.Hkv, c.Dk) or v.shape != (n, c.Hkv, c.Dv) or (c.Hkv > 1 and (k.stride(1) != c.Dk or v.stride(1) != c.Dv)):
         raise ValueError(f"k must be [n, {c.Hkv}, {c.Dk}] and v [n, {c.Hkv}, {c.Dv}], the heads of a row side by side")
-    _need_int32(dev, ("positions", positions, (n,)), ("sequences", sequences, (n,)))
+    _need_int32(dev, "positions", positions, (n,))
+    if sequences is not None:
+        _need_int32(dev, "sequences", sequences, (n,))
     if mass is not None:
         _need_mass(dev, "mass", mass, c.B, c.Hkv, 0)
-    st = lib().paep_cache_append(ctypes.byref(c), n, _ptr(k), _stride(k, 0), _ptr(v), _stride(v, 0), _ptr(k_pages), _ptr(v_pages),
+    st = lib().paep_cache_append(c.desc, n, _ptr(k), _stride(k, 0), _ptr(v), _stride(v, 0), _ptr(k_pages), _ptr(v_pages),
                                  _ptr(page_table), _ptr(sequences), _ptr(positions), _ptr(mass),
                                  0 if mass is None else mass.shape[2], _stream_ptr(stream))
     if st != 0:
@@ -688,26 +716,27 @@ def cache_evict(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.
     """Cut every sequence down to `budget` positions: each head keeps its last `recent` ones and, of those before them, the
     ones with the largest accumulated weight `mass` [B, Hkv, >= max_len]; they are copied, in order, to the pages of
     out_table [B, out_pages] int32 of the same pools, which must be free.  Shorter sequences are copied whole."""
-    c = _cache_desc(k_pages, v_pages, page_table)
-    dev, B, H = k_pages.device, c.B, c.Hkv
+    c = _cache(k_pages, v_pages, page_table)
+    dev, B, H = c.dev, c.B, c.Hkv
     if max_len is None:
-        max_len = c.max_pages * c.page_size
+        max_len = c.capacity
     _need_mass(dev, "mass", mass, B, H, max_len)
     if out_table.dim() != 2 or out_table.shape[0] != B:
         raise ValueError("out_table must be [B, out_pages]")
-    _need_int32(dev, ("lengths", lengths, (B,)), ("out_table", out_table, None))
+    _need_int32(dev, "lengths", lengths, (B,))
+    _need_int32(dev, "out_table", out_table, None)
     if budget < 1:
         raise ValueError("budget must be at least 1")
     if out is None:
         with _on(stream):
-            out = Eviction(torch.empty_like(lengths), torch.empty((B, H, budget), dtype=torch.int32, device=dev),
-                           torch.empty_like(mass))
+            out = Eviction(torch.empty_like(lengths), lengths.new_empty((B, H, budget)), torch.empty_like(mass))
     else:
-        _need_int32(dev, ("out.lengths", out.lengths, (B,)), ("out.kept", out.kept, (B, H, budget)))
+        _need_int32(dev, "out.lengths", out.lengths, (B,))
+        _need_int32(dev, "out.kept", out.kept, (B, H, budget))
         _need_mass(dev, "out.mass", out.mass, B, H, min(budget, max_len))
         if out.mass.data_ptr() == mass.data_ptr() or out.lengths.data_ptr() == lengths.data_ptr():
             raise ValueError("out.mass and out.lengths must be other buffers than mass and lengths")
-    st = lib().paep_cache_evict(ctypes.byref(c), max_len, budget, recent, _ptr(k_pages), _ptr(v_pages), _ptr(page_table),
+    st = lib().paep_cache_evict(c.desc, max_len, budget, recent, _ptr(k_pages), _ptr(v_pages), _ptr(page_table),
                                 _ptr(lengths), _ptr(mass), mass.shape[2], _ptr(out_table), out_table.shape[1], _ptr(out.kept),
                                 _ptr(out.mass), out.mass.shape[2], _ptr(out.lengths), _stream_ptr(stream))
     if st != 0:

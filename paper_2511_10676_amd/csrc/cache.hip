@@ -57,19 +57,23 @@ hipError_t launch_cache_append(const CacheView& c, int n, const void* k, long lo
 static constexpr int SEL_THREADS = 1024, SEL_WAVES = SEL_THREADS / 64;
 static constexpr int SEL_KEYS = 32;                  // masses of a thread at a time
 static constexpr int SEL_SPAN = SEL_THREADS * SEL_KEYS;
-static constexpr int SEL_COPIES = 8;                 // of every counter, a lane's by its number: most masses share a few digits
+static constexpr int SEL_BINS = 2 * SEL_THREADS;     // of a digit of 11 bits
+static constexpr int SEL_COPIES = 4;                 // of every counter, a lane's by its number: most masses share a few digits
 
 // A workgroup per sequence and head.  The (budget - recent)-th largest mass is found digit by digit on the ordered 32-bit
-// patterns (four histograms of 8 bits in LDS); everything above it is kept, and of its equals the lowest positions.  Up to
-// SEL_SPAN masses stay in registers from the first histogram to the last store; longer sequences are read again for each.
+// patterns (three histograms, 11, 11 and 10 bits, in LDS); everything above it is kept, and of its equals the lowest
+// positions.  Up to SEL_SPAN masses stay in registers from the first histogram to the last store; longer sequences are read
+// again for each.  What bounds it is the vector units of the one CU that a head has: 32493 masses of a head take 26 us, half
+// of it the histograms (four of 8 bits: 31 us; 76 us with the masses read from memory for each and a barrier per 1024).
 __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(
     int Hkv, int max_len, int budget, int recent, const int32_t* __restrict__ lengths, const float* __restrict__ mass,
     long long mass_stride, int32_t* __restrict__ kept, float* __restrict__ mass_out, long long mass_out_stride,
     int32_t* __restrict__ lengths_out)
 {
-    __shared__ uint32_t hist[256][SEL_COPIES], chosen[2];
-    __shared__ uint32_t counts[SEL_KEYS * SEL_WAVES];        // of a span, per 64 positions: above the threshold | at it << 16; then what is before
-    __shared__ uint32_t carry[2];
+    __shared__ __attribute__((aligned(16))) uint32_t hist[SEL_BINS][SEL_COPIES];
+    __shared__ uint32_t chosen[2], wave_sum[SEL_WAVES];
+    __shared__ uint32_t gt_bits[SEL_THREADS], eq_bits[SEL_THREADS];      // of a span, a bit per position: above the threshold, at it
+    __shared__ uint32_t wave_gt[SEL_WAVES], wave_eq[SEL_WAVES];
     const int b = blockIdx.x / Hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = clamped_length(lengths, b, max_len);
     const float* in = mass + (long long)blockIdx.x * mass_stride;
@@ -87,7 +91,9 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(
     for (int j = tid; j < recent; j += SEL_THREADS) { ids[best + j] = old + j; out[best + j] = in[old + j]; }
     if (best == 0) return;
 
-    uint32_t key[SEL_KEYS];                                  // of position p0 + u * SEL_THREADS + tid; 0, below every number's, where there is none
+    // key[u]: of position p0 + u * SEL_THREADS + tid.  Where there is none: 0, the lowest key, behind every position that has
+    // it, so it is never among the `best` <= old first ones and needs no test.
+    uint32_t key[SEL_KEYS];
     auto load = [&](long long p0) {
         float m[SEL_KEYS];
 #pragma unroll
@@ -96,110 +102,103 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(
             m[u] = in[p < old ? p : 0];
         }
 #pragma unroll
-        for (int u = 0; u < SEL_KEYS; ++u) key[u] = orderable(m[u]);
+        for (int u = 0; u < SEL_KEYS; ++u) key[u] = p0 + u * SEL_THREADS + tid < old ? orderable(m[u]) : 0u;
     };
     const bool whole = old <= SEL_SPAN;
     if (whole) load(0);
 
     uint32_t threshold = 0, need = best;                     // the threshold's digits so far, and its rank among the keys that share them
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = tid; i < 256 * SEL_COPIES; i += SEL_THREADS) (&hist[0][0])[i] = 0;
+#pragma unroll 1
+    for (int digit = 0; digit < 3; ++digit) {
+        const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, mask = digit == 2 ? 1023 : 2047;
+        const uint32_t within = digit == 0 ? 0xFFFFFFFFu : digit == 1 ? (1u << 21) - 1 : (1u << 10) - 1;     // keys that share the threshold's digits
+        for (int i = tid; i < SEL_BINS * SEL_COPIES; i += SEL_THREADS) (&hist[0][0])[i] = 0;
         __syncthreads();
         for (long long p0 = 0; p0 < old; p0 += SEL_SPAN) {
             if (!whole) load(p0);
-            const uint32_t within = shift == 24 ? 0xFFFFFFFFu : (1u << (shift + 8)) - 1u;      // keys that share the threshold's digits
 #pragma unroll
             for (int u = 0; u < SEL_KEYS; ++u) {
                 if (p0 + u * SEL_THREADS >= old) break;
-                if ((key[u] ^ threshold) <= within && p0 + u * SEL_THREADS + tid < old)
-                    atomicAdd(&hist[(key[u] >> shift) & 255u][lane % SEL_COPIES], 1u);
+                if ((key[u] ^ threshold) <= within) atomicAdd(&hist[(key[u] >> shift) & mask][lane % SEL_COPIES], 1u);
             }
         }
         __syncthreads();
-        if (tid < 256) {                                     // (a row's copies in an order that spreads over the banks)
-            uint32_t c = 0;
+        // thread t: the digits SEL_BINS - 1 - 2t and the one below; those above them are counted by the threads before it
+        uint32_t c[2];
 #pragma unroll
-            for (int i = 0; i < SEL_COPIES; ++i) c += hist[tid][(i + tid) % SEL_COPIES];
-            counts[tid] = c;
+        for (int i = 0; i < 2; ++i) {
+            const u32x4 h = *(const u32x4*)hist[SEL_BINS - 1 - 2 * tid - i];
+            c[i] = (h[0] + h[1]) + (h[2] + h[3]);
         }
+        uint32_t upto = c[0] + c[1];
+        for (int s = 1; s < 64; s <<= 1) {
+            const uint32_t o = __shfl_up(upto, s, 64);
+            if (lane >= s) upto += o;
+        }
+        if (lane == 63) wave_sum[wave] = upto;
         __syncthreads();
-        if (wave == 0) {                                     // lane l: digits 255 - 4l .. 252 - 4l
-            uint32_t c[4], sum = 0;
+        uint32_t before = upto - c[0] - c[1];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) { c[u] = counts[255 - 4 * lane - u]; sum += c[u]; }
-            uint32_t upto = sum;                             // inclusive over lanes
-            for (int s = 1; s < 64; s <<= 1) {
-                const uint32_t o = __shfl_up(upto, s, 64);
-                if (lane >= s) upto += o;
-            }
-            uint32_t before = upto - sum;
+        for (int w = 0; w < SEL_WAVES; ++w) before += w < wave ? wave_sum[w] : 0u;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                if (before < need && need <= before + c[u]) { chosen[0] = 255 - 4 * lane - u; chosen[1] = need - before; }
-                before += c[u];
-            }
+        for (int i = 0; i < 2; ++i) {
+            if (before < need && need <= before + c[i]) { chosen[0] = SEL_BINS - 1 - 2 * tid - i; chosen[1] = need - before; }
+            before += c[i];
         }
         __syncthreads();
         threshold |= chosen[0] << shift;
         need = chosen[1];
-        __syncthreads();
     }
-    // in ascending position: everything above the threshold and the first `need` at it
-    if (tid == 0) carry[0] = carry[1] = 0;
+    // in ascending position: everything above the threshold and the first `need` at it.  The span's positions become bits,
+    // thread t then has those of positions p0 + 32 t .. 32 t + 31.
+    uint32_t above = 0, equal = 0;                           // of the spans before
     for (long long p0 = 0; p0 < old; p0 += SEL_SPAN) {
         if (!whole) load(p0);
-#pragma unroll
-        for (int u = 0; u < SEL_KEYS; ++u) {
-            const bool there = p0 + u * SEL_THREADS + tid < old;
-            const uint32_t both = (uint32_t)__popcll(__ballot(there && key[u] > threshold)) |
-                                  (uint32_t)__popcll(__ballot(there && key[u] == threshold)) << 16;
-            if (lane == 0) counts[u * SEL_WAVES + wave] = both;
-        }
-        __syncthreads();
-        if (wave == 0) {                                     // what is before each 64 positions: lane l has 8 of them
-            constexpr int MINE = SEL_KEYS * SEL_WAVES / 64;
-            uint32_t c[MINE], sg = 0, se = 0;
-#pragma unroll
-            for (int i = 0; i < MINE; ++i) { c[i] = counts[lane * MINE + i]; sg += c[i] & 0xFFFFu; se += c[i] >> 16; }
-            uint32_t ug = sg, ue = se;
-            for (int s = 1; s < 64; s <<= 1) {
-                const uint32_t og = __shfl_up(ug, s, 64), oe = __shfl_up(ue, s, 64);
-                if (lane >= s) { ug += og; ue += oe; }
-            }
-            uint32_t g = ug - sg, e = ue - se;               // (up to 32768 each: 16 bits)
-#pragma unroll
-            for (int i = 0; i < MINE; ++i) {
-                counts[lane * MINE + i] = g | e << 16;
-                g += c[i] & 0xFFFFu;
-                e += c[i] >> 16;
-            }
-        }
-        __syncthreads();
-        const uint32_t g0 = carry[0], e0 = carry[1];
-        uint32_t ng = 0, ne = 0;
+        unsigned long long gt = 0, eq = 0;                   // lane u: of positions p0 + u * SEL_THREADS + wave * 64 ..
 #pragma unroll
         for (int u = 0; u < SEL_KEYS; ++u) {
             if (p0 + u * SEL_THREADS >= old) break;
-            const long long p = p0 + u * SEL_THREADS + tid;
-            const bool g = p < old && key[u] > threshold, e = p < old && key[u] == threshold;
-            const unsigned long long bg = __ballot(g), be = __ballot(e);
-            const uint32_t c = counts[u * SEL_WAVES + wave];
-            ng = g0 + (c & 0xFFFFu) + __builtin_amdgcn_mbcnt_hi((uint32_t)(bg >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)bg, 0));
-            ne = e0 + (c >> 16) + __builtin_amdgcn_mbcnt_hi((uint32_t)(be >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)be, 0));
-            if (g || (e && ne < need)) {
-                const uint32_t j = ng + min(ne, need);
-                ids[j] = (int32_t)p;
-                out[j] = in[p];
-            }
-            ng += g ? 1u : 0u;
-            ne += e ? 1u : 0u;
+            const unsigned long long bg = __ballot(key[u] > threshold), be = __ballot(key[u] == threshold);
+            gt = lane == u ? bg : gt;
+            eq = lane == u ? be : eq;
+        }
+        if (lane < SEL_KEYS) {
+            const int i = lane * (SEL_THREADS / 32) + wave * 2;
+            gt_bits[i] = (uint32_t)gt;
+            gt_bits[i + 1] = (uint32_t)(gt >> 32);
+            eq_bits[i] = (uint32_t)eq;
+            eq_bits[i + 1] = (uint32_t)(eq >> 32);
         }
         __syncthreads();
-        if (tid == SEL_THREADS - 1) {                        // (a further span follows a full one only)
-            carry[0] = ng;
-            carry[1] = ne;
+        uint32_t mine = gt_bits[tid], ties = eq_bits[tid];
+        const uint32_t ng = __popc(mine), ne = __popc(ties);
+        uint32_t g = ng, e = ne;                             // of the wave, up to this thread
+        for (int s = 1; s < 64; s <<= 1) {
+            const uint32_t og = __shfl_up(g, s, 64), oe = __shfl_up(e, s, 64);
+            if (lane >= s) { g += og; e += oe; }
         }
+        if (lane == 63) { wave_gt[wave] = g; wave_eq[wave] = e; }
+        __syncthreads();
+        g += above - ng;
+        e += equal - ne;
+#pragma unroll
+        for (int w = 0; w < SEL_WAVES; ++w) {
+            if (w < wave) { g += wave_gt[w]; e += wave_eq[w]; }
+            above += wave_gt[w];
+            equal += wave_eq[w];
+        }
+        for (uint32_t left = e < need ? need - e : 0; left > 0 && ties != 0; --left) {
+            mine |= ties & (0u - ties);
+            ties &= ties - 1;
+        }
+        for (uint32_t j = g + min(e, need); mine != 0; ++j, mine &= mine - 1)
+            ids[j] = (int32_t)(p0 + tid * 32 + __builtin_ctz(mine));
+        __syncthreads();
     }
+    // their masses (read again: a key has lost a zero's sign and what a NaN carries; and not above, where each would be waited for)
+    __syncthreads();
+#pragma unroll 4
+    for (int j = tid; j < best; j += SEL_THREADS) out[j] = in[ids[j]];
 }
 
 static constexpr int MOVE_THREADS = 256, MOVE_ROWS = 64, MOVE_PIECES = 8;
