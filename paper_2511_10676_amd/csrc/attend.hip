@@ -4,20 +4,25 @@
 //
 // Every key and value is needed once by the G query heads that share it, so what bounds the operator is reading the cache.
 // attend_kernel: a workgroup of four waves takes one chunk of one sequence's positions at one key-value head, for up to 16 of
-// its query heads; a wave takes every fourth tile of 32 positions (16 in fp32 storage).  Keys and values go from memory
-// straight into the registers of the matrix instructions, no LDS in between:
+// its query heads; a wave takes every fourth tile of 16 positions.  Keys and values go from memory straight into the
+// registers of the matrix instructions, no LDS in between:
 //   S^T = K Q^T   a wave's operand A is 16 keys, lane (m, g) holding 16 bytes of key m: four lanes fetch 64 contiguous bytes.
 //                 Lane (m, g) of the result holds head m's scores of keys 4g .. 4g + 3, which is operand B of the second
-//                 product as it stands, if its summation index runs over keys in that order:
-//   O^T = V^T P^T operand A wants 8 keys of one dimension in a lane.  Lane (c, g) fetches dimensions 8c .. 8c + 7 of the
-//                 8 keys that its lane group g holds (16 lanes read a whole row), and one byte permutation per register
-//                 transposes the 8 x 8 block inside the lane.  Row c of the j-th of 8 products is dimension 8c + j.
+//                 product as it stands:
+//   O^T = V^T P^T operand A wants 4 keys of one dimension in a lane.  Lane (c, g) fetches dimensions 8c .. 8c + 7 of the
+//                 4 keys that its lane group g holds (16 lanes read a whole row), and one byte permutation per register
+//                 transposes the block inside the lane.  Row c of the j-th of 8 products is dimension 8c + j.
 // (fp32 storage: the same with 16-byte pieces of 4 and the 16x16x4 instruction, key by key.)  The running maximum and sum are
-// per lane, one head each, and the accumulated O is rescaled in place, where a maximum grew, without any exchange between lanes.
-// P is multiplied as two bf16 parts (16 bits of it): the second instruction costs nothing next to the loads, and the result
-// keeps the accuracy of fp32 probabilities.
-// The next tile's keys are requested once this tile's are multiplied, the next values likewise, so that a wave always has
-// a tile in flight.  Waves are joined in LDS, chunks by attend_join_kernel, in a fixed order.
+// per lane, one head each, and the accumulated O is rescaled in place, where a maximum grew, without any exchange between
+// lanes.  P is multiplied as two bf16 parts (16 bits of it): the second instruction costs nothing next to the loads, and the
+// result keeps the accuracy of fp32 probabilities.
+// The next tile's keys are requested once this tile's are multiplied, the next values likewise, so that a wave always has a
+// tile in flight.  Tiles of 16 positions, not of 32, leave registers for three workgroups on a CU instead of two (131071
+// positions 58 -> 56 us, 32 heads on one key-value head of width 256 56 -> 48 us), and one block of 16 query heads to a
+// workgroup, not two, for two (32 heads of width 256 94 -> 55 us, of width 128 32 -> 25 us).  Waves are joined in LDS, chunks by
+// attend_join_kernel, in a fixed order.
+// Measured: 131071 positions of 4 key-value heads of 128 56 us (4.7 TB/s, 5.3 without the join's launch); 61 sequences of
+// 17 to 8192 positions, 8 heads, with mass 104 us.
 #include <type_traits>
 
 #include "cache_device.h"
@@ -25,6 +30,7 @@
 namespace paep {
 
 static constexpr int ATT_THREADS = 256, ATT_WAVES = ATT_THREADS / 64;
+static constexpr int TILE = 16;                  // positions of a wave at a time
 static constexpr int TABLE = 2048;               // page-table entries in LDS at a time
 static constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.69314718055994531f;
 
@@ -68,11 +74,9 @@ __device__ __forceinline__ float origin(float m) { return m == -__builtin_inff()
 // KS: 16-byte steps of four lanes that cover a key; VB: blocks of 16 lanes x 16 bytes that cover a value;
 // MASS: the scores are kept for attend_join_kernel
 template <bool BF16, int KS, int VB, bool MASS>
-__global__ __launch_bounds__(ATT_THREADS, VB == (BF16 ? 1 : 2) && KS <= (BF16 ? 4 : 8) ? 2 : 1) void attend_kernel(AttendArgs a, AttendPlan pl)
+__global__ __launch_bounds__(ATT_THREADS, BF16 ? (VB == 1 && KS <= 4 ? 3 : 2) : (VB == 2 && KS <= 8 ? 2 : 1)) void attend_kernel(AttendArgs a, AttendPlan pl)
 {
     constexpr int PER = BF16 ? 8 : 4;            // elements of a 16-byte piece
-    constexpr int KT = BF16 ? 2 : 1;             // 16-key blocks of a tile
-    constexpr int TILE = 16 * KT, NK = 4 * KT;   // keys of a tile; of them in a lane
     __shared__ __attribute__((aligned(16))) union {
         int pages[TABLE + 1];                    // while the positions are walked
         f32x4 o[ATT_WAVES][PER][64];             // the waves' results, a block of dimensions at a time
@@ -122,8 +126,8 @@ __global__ __launch_bounds__(ATT_THREADS, VB == (BF16 ? 1 : 2) && KS <= (BF16 ? 
     const unsigned char* kbase = a.c.k + kvh * a.c.k_head;
     const unsigned char* vbase = a.c.v + kvh * a.c.v_head;
     const int slots = (1 << a.c.page_shift) - 1;
-    u32x4 kf[KT][KS], vf[NK][VB];
-    uint32_t live = 0;                           // which of the lane's NK keys take part
+    u32x4 kf[KS], vf[4][VB];
+    uint32_t live = 0;                           // which of the lane's 4 keys take part
 
     const long long stretch = (long long)TABLE << a.c.page_shift;        // positions whose page-table entries fit in LDS
     for (long long p0 = begin; p0 < end; p0 += stretch) {
@@ -145,36 +149,28 @@ __global__ __launch_bounds__(ATT_THREADS, VB == (BF16 ? 1 : 2) && KS <= (BF16 ? 
             return base + max(page, 0) * page_bytes + (page < 0 ? 0 : pos & slots) * slot_bytes;
         };
         auto load_k = [&](int p) {
-            int page[KT];
+            const unsigned char* at = row_at(kbase, a.c.k_page, a.c.k_slot, page_of(p + m), p + m);
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt) page[kt] = page_of(p + kt * 16 + m);
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                const unsigned char* at = row_at(kbase, a.c.k_page, a.c.k_slot, page[kt], p + kt * 16 + m);
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    const int piece = ks * 4 + g;
-                    kf[kt][ks] = *(const u32x4*)(at + (piece * PER < a.c.Dk ? piece : 0) * 16);
-                }
+            for (int ks = 0; ks < KS; ++ks) {
+                const int piece = ks * 4 + g;
+                kf[ks] = *(const u32x4*)(at + (piece * PER < a.c.Dk ? piece : 0) * 16);
             }
         };
         auto load_v = [&](int p) {
-            int page[NK];
+            const int pos = p + g * 4;
+            int page[4];
             if (a.c.page_shift >= 2) {           // four neighbours are on one page
+                const int i = (pos >> a.c.page_shift) - page0, one = lds.pages[min(max(i, 0), last_entry)];
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt) {
-                    const int pos = p + kt * 16 + g * 4, i = (pos >> a.c.page_shift) - page0, one = lds.pages[min(max(i, 0), last_entry)];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) page[kt * 4 + j] = (int)(pos + j >= r.start) & (int)(pos + j < stop) & (int)(one >= 0) ? one : -1;
-                }
+                for (int j = 0; j < 4; ++j) page[j] = (int)(pos + j >= r.start) & (int)(pos + j < stop) & (int)(one >= 0) ? one : -1;
             } else {
 #pragma unroll
-                for (int j = 0; j < NK; ++j) page[j] = page_of(p + (j >> 2) * 16 + g * 4 + (j & 3));
+                for (int j = 0; j < 4; ++j) page[j] = page_of(pos + j);
             }
             live = 0;
 #pragma unroll
-            for (int j = 0; j < NK; ++j) {
-                const unsigned char* at = row_at(vbase, a.c.v_page, a.c.v_slot, page[j], p + (j >> 2) * 16 + g * 4 + (j & 3));
+            for (int j = 0; j < 4; ++j) {
+                const unsigned char* at = row_at(vbase, a.c.v_page, a.c.v_slot, page[j], pos + j);
                 live |= page[j] < 0 ? 0u : 1u << j;
 #pragma unroll
                 for (int vb = 0; vb < VB; ++vb) {
@@ -190,48 +186,39 @@ __global__ __launch_bounds__(ATT_THREADS, VB == (BF16 ? 1 : 2) && KS <= (BF16 ? 
         for (; p < stop; p += ATT_WAVES * TILE) {
             if (a.c.Dk != KS * 4 * PER) {        // pieces past the key's end
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt)
+                for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-                    for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) kf[kt][ks][i] = (ks * 4 + g) * PER < a.c.Dk ? kf[kt][ks][i] : 0u;
+                    for (int i = 0; i < 4; ++i) kf[ks][i] = (ks * 4 + g) * PER < a.c.Dk ? kf[ks][i] : 0u;
             }
-            f32x4 s[KT];
+            f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                s[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) s[kt] = product<BF16>(kf[kt][ks], qf[ks], s[kt]);
-            }
+            for (int ks = 0; ks < KS; ++ks) s = product<BF16>(kf[ks], qf[ks], s);
             const uint32_t now = live;
             const int next = p + ATT_WAVES * TILE;
             load_k(next);
             __builtin_amdgcn_sched_barrier(0);   // requested here, not where they are used
 
-            if (!__all(now == (1u << NK) - 1)) {
+            if (!__all(now == 15u)) {
                 // what stands in a row that does not take part may be anything: no NaN of it may reach the sums
 #pragma unroll
-                for (int j = 0; j < NK; ++j)
+                for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int vb = 0; vb < VB; ++vb)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) vf[j][vb][i] = (now >> j) & 1u ? vf[j][vb][i] : 0u;
             }
-            float z[NK], most = -__builtin_inff();
+            float z[4], most = -__builtin_inff();
 #pragma unroll
-            for (int j = 0; j < NK; ++j) {
-                z[j] = (now >> j) & 1u ? s[j >> 2][j & 3] * factor : -__builtin_inff();
+            for (int j = 0; j < 4; ++j) {
+                z[j] = (now >> j) & 1u ? s[j] * factor : -__builtin_inff();
                 most = fmaxf(most, z[j]);
             }
             if constexpr (MASS) {
-                // (stores without a branch, which the counting of outstanding loads would have to assume taken: what lies
+                // (a store without a branch, which the counting of outstanding loads would have to assume taken: what lies
                 // behind the head's row of the chunk, or past the group, is dropped by its offset)
-#pragma unroll
-                for (int kt = 0; kt < KT; ++kt) {
-                    const int at = p + kt * 16 + g * 4 - begin;
-                    __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(z[4 * kt]), __float_as_uint(z[4 * kt + 1]), __float_as_uint(z[4 * kt + 2]), __float_as_uint(z[4 * kt + 3])},
-                                                           kept, at < pl.chunk ? (m * pl.chunk + at) * 4 : 0x7FFFFFF0, 0, 0);
-                }
+                const int at = p + g * 4 - begin;
+                __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(z[0]), __float_as_uint(z[1]), __float_as_uint(z[2]), __float_as_uint(z[3])},
+                                                       kept, at < pl.chunk ? (m * pl.chunk + at) * 4 : 0x7FFFFFF0, 0, 0);
             }
             most = fmaxf(most, __shfl_xor(most, 16, 64));
             most = fmaxf(most, __shfl_xor(most, 32, 64));
@@ -247,16 +234,16 @@ __global__ __launch_bounds__(ATT_THREADS, VB == (BF16 ? 1 : 2) && KS <= (BF16 ? 
                         for (int i = 0; i < 4; ++i) o[vb][j][i] *= keep;
             }
             const float at = origin(top);
-            float e[NK];
+            float e[4];
 #pragma unroll
-            for (int j = 0; j < NK; ++j) {
+            for (int j = 0; j < 4; ++j) {
                 e[j] = exp2_(z[j] - at);
                 sum += e[j];
             }
             if constexpr (BF16) {
-                u32x4 high, low;                 // P in two parts
+                u32x2 high, low;                 // P in two parts
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < 2; ++i) {
                     high[i] = pack_bf16x2(e[2 * i], e[2 * i + 1]);
                     low[i] = pack_bf16x2(e[2 * i] - __uint_as_float(high[i] << 16), e[2 * i + 1] - __uint_as_float(high[i] & 0xFFFF0000u));
                 }
@@ -264,11 +251,13 @@ __global__ __launch_bounds__(ATT_THREADS, VB == (BF16 ? 1 : 2) && KS <= (BF16 ? 
                 for (int vb = 0; vb < VB; ++vb)
 #pragma unroll
                     for (int j = 0; j < PER; ++j) {
-                        u32x4 t;                 // dimension 8c + j of the lane's 8 keys
+                        u32x2 t;                 // dimension 8c + j of the lane's 4 keys
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
+                        for (int i = 0; i < 2; ++i)
                             t[i] = __builtin_amdgcn_perm(vf[2 * i + 1][vb][j >> 1], vf[2 * i][vb][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
-                        o[vb][j] = product<true>(t, low, product<true>(t, high, o[vb][j]));
+                        const short4v x = __builtin_bit_cast(short4v, t);
+                        o[vb][j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x, __builtin_bit_cast(short4v, high), o[vb][j], 0, 0, 0);
+                        o[vb][j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x, __builtin_bit_cast(short4v, low), o[vb][j], 0, 0, 0);
                     }
             } else {
 #pragma unroll
@@ -448,12 +437,12 @@ __global__ __launch_bounds__(JOIN_THREADS) void attend_join_kernel(AttendArgs a,
 
 // ---------------------------------------------------------------------------
 
-// How the positions are cut.  Two workgroups run on a CU, so the longest sequences are cut into enough chunks that there are
-// 512 workgroups, if a chunk then still has 256 positions (two tiles per wave): a chunk of 128 costs a join that takes
-// longer than it saves (one sequence of 151 positions: 8.8 us whole, 11.1 us in two chunks).  With several sequences a chunk has at
-// most 512 positions, because their lengths differ and the host does not know them: 61 sequences of 17 to 8192 positions
-// take 90 us in chunks of 512 and 95 us in chunks of 2048 (with mass 106 and 116), 61 of 1400 positions 82 and 74 us.
-// One sequence: 2048 (131071 positions: 58 us, 62 us in chunks of 512).
+// How the positions are cut.  The longest sequences are cut into enough chunks that there are two workgroups for every CU, if
+// a chunk then still has 256 positions (four tiles per wave): a smaller one costs a join that takes longer than it saves (one
+// sequence of 151 positions 8.1 us whole, 10.8 in two chunks; 131071 positions 56 us, for three workgroups per CU 61).  With several
+// sequences a chunk has at most 512 positions, because their lengths differ and the host does not know them (61 sequences of
+// 17 to 8192 positions with mass: 104 us, 116 in chunks of 2048; 61 of 1400 each 77 us, and 70 in one chunk each); one sequence
+// is cut into chunks of up to 2048.
 static AttendPlan plan_of(const AttendArgs& a)
 {
     constexpr int TARGET = 512, LEAST = 256;
@@ -461,7 +450,7 @@ static AttendPlan plan_of(const AttendArgs& a)
     pl.G = a.Hq / a.c.Hkv;
     pl.head_blocks = (pl.G + 15) / 16;
     pl.rows = a.c.B * a.c.Hkv;
-    const int step = ATT_WAVES * (a.c.dtype == 1 ? 32 : 16);     // positions that a workgroup's waves take at once
+    constexpr int step = ATT_WAVES * TILE;                       // positions that a workgroup's waves take at once
     const long long items = pl.rows > 0 ? (long long)pl.rows * pl.head_blocks : 1;
     long long chunk = ((long long)a.max_len * items + TARGET - 1) / TARGET;
     long long most = a.c.B > 1 ? 512 : 2048;
