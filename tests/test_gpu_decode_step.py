@@ -561,3 +561,18 @@ def test_decode_step_in_a_graph():
         for a, b in ((eager["at"].out, rec["at"].out), (eager["at"].lse, rec["at"].lse), (eager["mass"], rec["mass"]), (eager["k"], rec["k"]),
                      (eager["moe"].y, rec["moe"].y), (eager["moe"].idx, rec["moe"].idx), (eager["pos"], rec["pos"])):
             assert torch.equal(a, b), i
+
+
+def test_example_runs_the_operators_together():
+    import importlib.util
+    import os
+    import sys
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "decode_step.py")
+    spec = importlib.util.spec_from_file_location("decode_step_example", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    argv, sys.argv = sys.argv, ["decode_step.py", "--steps", "100"]      # past the first eviction
+    try:
+        assert example.main() > 0.5                          # by chance: 12 of 128
+    finally:
+        sys.argv = argv
