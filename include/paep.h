@@ -496,7 +496,7 @@ size_t paep_moe_workspace_bytes(const paep_moe_desc *desc);
  *     z = Wg x_t (+ bg), fp32;   idx[t] = the k highest of z, as in paep_predict
  *     p[t,j] = the softmax of z at idx[t,j], or what prob says;  probs = p
  *     u_j = W13[idx_j][0..f) x_t,   w_j = W13[idx_j][f..2f) x_t
- *     h_j = p_j act(u_j) w_j              in bf16 storage held as two bf16 parts, 16 bits of it
+ *     h_j = p_j act(u_j) w_j              fp32
  *     y_t = residual_t + sum_j W2[idx_j] h_j        fp32 sums, rounded once to dtype
  *   x_dev [T][d], Wg_dev [E][d], bg_dev [E] or NULL, W13_dev [E][2f][d] (the f
  *   gate rows, then the f others), W2_dev [E][d][f], residual_dev [T][d] or NULL

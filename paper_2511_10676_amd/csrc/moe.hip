@@ -9,9 +9,10 @@
 //   select_kernel   adds the slices, softmax and top-k with the predictor's own routines (or takes a given selection), and
 //                   lists the active experts and who picked them
 //   up_kernel       16 gate rows and the 16 rows beside them of one expert over all of d, for the tokens that picked it: the
-//                   four waves split d.  h goes to the workspace, already weighed by p; in bf16 storage as two bf16 parts,
-//                   high and low (16 bits of it: a rounding to 8 bits would cost the result as much as its own)
-//   down_kernel     16 rows of d over all active experts: the eight waves split (expert, part of f); sums per token in LDS
+//                   four waves split d.  h goes to the workspace in fp32, already weighed by p
+//   down_kernel     16 rows of d over all active experts: the eight waves split (expert, part of f); sums per token in LDS.
+//                   With h in 16 bits (two bf16 parts, stored) sums that cancel had fewer right bits than y can hold; taking all
+//                   24 bits of it apart here costs 1 to 3 % of the layer
 //   sum_kernel      where two or more workgroups share 16 rows
 // A fragment of 16 rows x 64 bytes is fetched with four neighbouring lanes on 64 contiguous bytes of a row, and a fixed lane
 // permutation puts it into the operand layout (as in predict_decode.hip).
@@ -260,7 +261,7 @@ __global__ __launch_bounds__(SELECT_THREADS) void select_kernel(MoeArgs a, const
 }
 
 // ---------------------------------------------------------------------------
-// h: [T * k][f], fp32, or the bf16 planes high and low one after the other
+// h: [T * k][f], fp32
 // ---------------------------------------------------------------------------
 static constexpr int UP_THREADS = 256;
 
@@ -365,16 +366,7 @@ template <bool BF16, int NT, int U> struct UpWave {
                 v[c] = weight * apply_act(gate, a.act) * up;
             }
             const long long at = (long long)p * a.f + unit;
-            if constexpr (BF16) {
-                const u32x2 hi = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-                float lo[4];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) lo[c] = v[c] - __uint_as_float(c & 1 ? hi[c >> 1] & 0xFFFF0000u : hi[c >> 1] << 16);
-                *(u32x2*)((uint16_t*)h + at) = hi;
-                *(u32x2*)((uint16_t*)h + (long long)a.T * a.k * a.f + at) = u32x2{pack_bf16x2(lo[0], lo[1]), pack_bf16x2(lo[2], lo[3])};
-            } else {
-                *(f32x4*)((float*)h + at) = f32x4{v[0], v[1], v[2], v[3]};
-            }
+            *(f32x4*)((float*)h + at) = f32x4{v[0], v[1], v[2], v[3]};
         }
         __syncthreads();
     }
@@ -451,60 +443,61 @@ template <bool BF16> __device__ __forceinline__ void write_y(const MoeArgs& a, l
     }
 }
 
-// One unit: steps s0 .. s0 + U - 1 of expert slot `slot`, into the wave's sums ysum[t][16].  NT: blocks of columns; a column
-// is a token, in bf16 storage a token's high (columns 0..7 of a block) or low part (8..15).
-template <bool BF16, int NT, int U> struct DownUnit {
-    static constexpr int TOK = BF16 ? 8 : 16;        // tokens of a block
-    u32x4 fw[U], fh[U][NT];
+// One unit: steps s0 .. s0 + U - 1 of expert slot `slot`, for 16 of its tokens, into the wave's sums ysum[t][16].  h is read in the
+// order of the operand: lane (n, c) has token n's values beside piece c of the weights.  In bf16 storage they are multiplied as
+// three bf16 parts of 8 bits, cut off and not rounded: exactly the 24 bits of an fp32 number, and a finite h has finite parts.
+template <bool BF16, int U> struct DownUnit {
+    static constexpr int TOK = 16, H = BF16 ? 2 : 1;     // tokens of a block; pieces of h beside a piece of the weights
+    u32x4 fw[U], fh[U][H];
 
-    __device__ __forceinline__ void load(const MoeArgs& a, const Picked& ls, const void* h, int slot, int block0, int s0, int row0, int lane)
+    // WEIGHTS: both; else h only, of a further block for the weights that are there
+    template <bool WEIGHTS> __device__ __forceinline__ void load(const MoeArgs& a, const Picked& ls, const void* h, int slot, int block, int s0, int row0, int lane)
     {
         const int row_bytes = a.f * (BF16 ? 2 : 4), row = lane >> 2, lane_off = (lane & 3) * 16;
         const Slot s(ls.slot[slot]);
         const Rows w = rows_at((const unsigned char*)a.W2 + ((long long)s.expert * a.d + row0) * row_bytes, (long long)min(a.d - row0, 16) * row_bytes);
         const Rows hr = rows_at(h, (long long)a.T * a.k * a.f * 4);
-        int hrow[NT];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int n = (block0 + nt) * TOK + (row & (TOK - 1));
-            hrow[nt] = n < s.tokens ? (ls.position[s.first + n] + (BF16 && row >= TOK ? a.T * a.k : 0)) * row_bytes : NOWHERE;
-        }
+        const int n = block * TOK + (lane & 15), hrow = n < s.tokens ? ls.position[s.first + n] * a.f * 4 : NOWHERE;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int off = (s0 + u) * STEP + lane_off;
-            fw[u] = piece(w, row * row_bytes, off, row_bytes);
+            if constexpr (WEIGHTS) fw[u] = piece(w, row * row_bytes, (s0 + u) * STEP + lane_off, row_bytes);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) fh[u][nt] = piece(hr, hrow[nt], off, row_bytes);
+            for (int i = 0; i < H; ++i) fh[u][i] = piece(hr, hrow, ((s0 + u) * STEP + (lane >> 4) * 16) * H + i * 16, a.f * 4);
         }
     }
 
-    __device__ __forceinline__ void add(const MoeArgs& a, const Picked& ls, int slot, int block0, int lane, float* ysum) const
+    __device__ __forceinline__ void add(const MoeArgs& a, const Picked& ls, int slot, int block, int lane, float* ysum) const
     {
-        f32x4 acc[NT];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) acc[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f}, rest = acc;       // (rest: of the second and third parts)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const u32x4 wo = to_operand(fw[u], lane);
+            if constexpr (BF16) {
+                float left[8];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) acc[nt] = product<BF16>(wo, to_operand(fh[u][nt], lane), acc[nt]);
+                for (int i = 0; i < 8; ++i) left[i] = __uint_as_float(fh[u][i >> 2][i & 3]);
+#pragma unroll
+                for (int part = 0; part < 3; ++part) {
+                    u32x4 x;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_perm(__float_as_uint(left[2 * i + 1]), __float_as_uint(left[2 * i]), 0x07060302u);
+                    if (part == 0) acc = product<BF16>(wo, x, acc);
+                    else           rest = product<BF16>(wo, x, rest);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) left[i] -= __uint_as_float(__float_as_uint(left[i]) & 0xFFFF0000u);
+                }
+            } else {
+                acc = product<BF16>(wo, fh[u][0], acc);
+            }
         }
         const Slot s(ls.slot[slot]);
-        const int col = lane & 15;
+        const int n = block * TOK + (lane & 15);
+        if (n < s.tokens) {
+            f32x4* y = (f32x4*)(ysum + (ls.position[s.first + n] / a.k) * 16 + 4 * (lane >> 4));
+            f32x4 v = *y;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            if constexpr (BF16) {                    // low part onto high part
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[nt][i] += __shfl_xor(acc[nt][i], 8, 64);
-            }
-            const int n = (block0 + nt) * TOK + col;
-            if (col < TOK && n < s.tokens) {
-                f32x4* y = (f32x4*)(ysum + (ls.position[s.first + n] / a.k) * 16 + 4 * (lane >> 4));
-                f32x4 v = *y;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] += acc[nt][i];
-                *y = v;
-            }
+            for (int i = 0; i < 4; ++i) v[i] += BF16 ? acc[i] + rest[i] : acc[i];
+            *y = v;
         }
     }
 };
@@ -523,24 +516,23 @@ __global__ __launch_bounds__(DOWN_THREADS, 2) void down_kernel(MoeArgs a, const 
     for (int i = tid; i < a.T * a.k; i += DOWN_THREADS) ls.position[i] = lists->position[i];
     __syncthreads();
     float* ysum = ysums + wave * a.T * 16;
-    constexpr int U = 8, TOK = BF16 ? 8 : 16;
+    constexpr int U = BF16 ? 6 : 8, TOK = DownUnit<BF16, U>::TOK;       // (bf16, 61 tokens: 7 steps 244 us, 8 238, 6 237)
     const int nsteps = (a.f * (BF16 ? 2 : 4) + STEP - 1) / STEP, pieces = (nsteps + U - 1) / U, units = n * pieces, stride = DOWN_WAVES * parts;
 
-    DownUnit<BF16, 1, U> ring[2];
+    DownUnit<BF16, U> ring[2];
     int i = part * DOWN_WAVES + wave;
-    if (i < units) ring[0].load(a, ls, h, i / pieces, 0, i % pieces * U, row0, lane);
+    if (i < units) ring[0].template load<true>(a, ls, h, i / pieces, 0, i % pieces * U, row0, lane);
     for (; i < units; i += 2 * stride)
         static_for<2>([&](auto b_c) {
             constexpr int b = decltype(b_c)::value;
             const int now = i + b * stride, next = now + stride;
-            if (next < units) ring[1 - b].load(a, ls, h, next / pieces, 0, next % pieces * U, row0, lane);
+            if (next < units) ring[1 - b].template load<true>(a, ls, h, next / pieces, 0, next % pieces * U, row0, lane);
             if (now < units) {
                 const int slot = now / pieces, tokens = Slot(ls.slot[slot]).tokens;
                 ring[b].add(a, ls, slot, 0, lane, ysum);
-                for (int block = 1; block * TOK < tokens; ++block) {                 // more tokens: the weights are in a cache by now
-                    DownUnit<BF16, 1, U> more;
-                    more.load(a, ls, h, slot, block, now % pieces * U, row0, lane);
-                    more.add(a, ls, slot, block, lane, ysum);
+                for (int block = 1; block * TOK < tokens; ++block) {
+                    ring[b].template load<false>(a, ls, h, slot, block, now % pieces * U, row0, lane);
+                    ring[b].add(a, ls, slot, block, lane, ysum);
                 }
             }
         });
@@ -572,11 +564,11 @@ template <bool BF16> __global__ __launch_bounds__(256) void sum_kernel(MoeArgs a
 
 static int row_steps(const MoeArgs& a, int n) { return (n * (a.dtype == PAEP_BF16 ? 2 : 4) + STEP - 1) / STEP; }
 static int router_slices(const MoeArgs& a) { return (row_steps(a, a.d) + ROUTER_STEPS - 1) / ROUTER_STEPS; }
-static size_t h_bytes(const MoeArgs& a) { return ((size_t)a.T * a.k * a.f * 4 + 15) & ~(size_t)15; }      // two bf16 planes or one of fp32
+static size_t h_bytes(const MoeArgs& a) { return ((size_t)a.T * a.k * a.f * 4 + 15) & ~(size_t)15; }
 
 static size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 // Workgroups that share 16 rows of d: enough for one per CU (a workgroup's registers leave room for no second), unless a wave would
-// have fewer than 8 units -- the sums' launch then costs what the other CUs gain (one token, 8 experts of 2048 x 768: 31 us
+// have fewer than 64 steps -- the sums' launch then costs what the other CUs gain (one token, 8 experts of 2048 x 768: 31 us
 // both ways; 61 tokens of 64 experts 243 us in two parts, 302 in one; more parts than CUs: 265).
 static int down_parts(const MoeArgs& a)
 {

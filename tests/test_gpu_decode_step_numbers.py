@@ -48,3 +48,27 @@ def test_attend_multiplies_probabilities_of_32_bits(n, where, dtype):
     tol = 16 * R.U * size / (1.0 + 2.0 * e[:, None]) + (R.BF16 if dtype == "bf16" else 4 * R.U) * np.abs(want)
     off = np.abs(_np(got.out)[0].astype(np.float64) - want)
     assert (off <= tol).all(), (off / tol).max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,f", [(1, 8), (5, 40), (16, 8), (40, 72), (64, 1000)])
+def test_moe_experts_multiply_hidden_values_of_32_bits(T, f, dtype):
+    """Token t has the weights p, r at experts 1 and 2, whose hidden values are p (unit 0) and r (units 0 and f - 1): gate and
+    other rows are exactly 1 there.  Row t of the second matrices is 1 and -v1, -v2 with v1 + v2 close to p / r: the sum all but
+    cancels.  Products are exact, about 8 sums of terms up to p round: 8 U p.  A hidden value of 16 bits is off by up to 64 U p."""
+    E, d = 4, max(16, -(-T // 8) * 8)
+    g = np.random.default_rng(T)
+    p, r = (g.uniform(0.5, 1.0, T).astype(np.float32).astype(np.float64) for _ in range(2))
+    x, W13, W2 = np.zeros((T, d)), np.zeros((E, 2 * f, d)), np.zeros((E, d, f))
+    x[:, 3] = 1.0
+    W13[1:3, [0, f - 1, f, 2 * f - 1], 3] = 1.0
+    high, low = _two_parts(p / r)
+    W2[1, :T, 0], W2[2, :T, 0], W2[2, :T, f - 1] = 1.0, -high, -low
+    idx = _i32(np.tile([1, 2], (T, 1)))
+    got = B.moe_experts(_to(x, dtype), _to(W13, dtype), _to(W2, dtype), idx, _to(np.stack([p, r], 1), "f32"), act="none")
+    torch.cuda.synchronize()
+    want = p[:, None] - r[:, None] * (high + low)[None]                                # [token, row]
+    tol = 8 * R.U * np.maximum(p[:, None], r[:, None] * (high + low)[None]) + (R.BF16 if dtype == "bf16" else 2 * R.U) * np.abs(want)
+    off = np.abs(_np(got)[:, :T].astype(np.float64) - want)
+    assert (off <= tol).all(), (off / tol).max()
+    assert not _np(got)[:, T:].any()
