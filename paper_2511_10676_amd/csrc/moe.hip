@@ -496,7 +496,11 @@ template <bool BF16, int U> struct DownUnit {
             f32x4* y = (f32x4*)(ysum + (ls.position[s.first + n] / a.k) * 16 + 4 * (lane >> 4));
             f32x4 v = *y;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] += BF16 ? acc[i] + rest[i] : acc[i];
+            for (int i = 0; i < 4; ++i) {
+                // where a weight or an h is infinite, the first part alone has the outcome: it has h's sign and is 0 only if h is
+                // (a later part, 0 or of the other sign, makes NaN of it)
+                v[i] += BF16 && __builtin_isfinite(acc[i]) ? acc[i] + rest[i] : acc[i];
+            }
             *y = v;
         }
     }

@@ -72,3 +72,62 @@ def test_moe_experts_multiply_hidden_values_of_32_bits(T, f, dtype):
     off = np.abs(_np(got)[:, :T].astype(np.float64) - want)
     assert (off <= tol).all(), (off / tol).max()
     assert not _np(got)[:, T:].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,f,residual", [(1, 8, False), (7, 200, True), (16, 1000, False), (40, 72, True), (64, 1000, True)])
+def test_moe_experts_with_infinite_weights(T, f, residual, dtype):
+    """Infinite entries of the second matrix, and hidden values that are infinite, or finite and above the largest bf16
+    number: every row of y is what the formula gives, and where that is finite, as close as ever."""
+    E, d, k = 6, 64, 2
+    g = np.random.default_rng(T + f)
+    x = _storage(g.standard_normal((T, d)), dtype)
+    W13 = _storage(g.standard_normal((E, 2 * f, d)) / np.sqrt(d), dtype)
+    W2 = _storage(g.standard_normal((E, d, f)) / np.sqrt(f), dtype)
+    idx = np.stack([g.permutation(E - 1)[:k] for _ in range(T)])
+    idx[0] = [0, 1]
+    probs = g.uniform(0.2, 0.8, (T, k)).astype(np.float32)
+    res = _storage(g.standard_normal((T, d)), dtype) if residual else None
+    finite, tol = R.experts(x, W13, W2, idx, probs, "silu", res, dtype == "bf16")
+    bad = W2.copy()
+    bad[0, 5, 3], bad[1, 5, f - 1], bad[1, 9, 0] = np.inf, np.inf, -np.inf
+    bad[2, 9, 2], bad[3, 63, f // 2], bad[4, 17, 1] = np.inf, np.nan, -np.inf
+    want = np.zeros((T, d)) if res is None else res.astype(np.float64).copy()
+    for t in range(T):
+        for j in range(k):
+            u = W13[idx[t, j]].astype(np.float64) @ x[t].astype(np.float64)
+            with np.errstate(invalid="ignore"):
+                want[t] += bad[idx[t, j]].astype(np.float64) @ (probs[t, j] * R.act(u[:f], "silu") * u[f:])
+    got = B.moe_experts(_to(x, dtype), _to(W13, dtype), _to(bad, dtype), _i32(idx), _to(probs, "f32"),
+                        residual=None if res is None else _to(res, dtype))
+    torch.cuda.synchronize()
+    y = _np(got).astype(np.float64)
+    here = np.isfinite(want)
+    assert not here.all() and here.any()
+    assert np.array_equal(y[~here], want[~here], equal_nan=True)
+    assert np.allclose(want[here], finite[here], rtol=1e-9, atol=1e-12) and (np.abs(y - finite)[here] <= tol[here]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [3, 40])
+def test_moe_experts_with_infinite_hidden_values(T, dtype):
+    """Hidden values p * 2^64 * u: infinite for u = 2^64 and p = 1, finite for p = 0.9985, where the nearest bf16 number is infinity."""
+    E, d, f = 3, 64, 24
+    x, W13, W2 = np.zeros((T, d)), np.zeros((E, 2 * f, d)), np.zeros((E, d, f))
+    x[:, 0] = 1.0
+    W13[:, 4, 0] = 2.0 ** 64                              # gate row 4; its other row:
+    W13[0, f + 4, 0], W13[1, f + 4, 0] = 2.0 ** 64, -2.0 ** 64
+    W2[:, :, 4] = 2.0 ** -10
+    W2[:, 1, 4] = -2.0 ** -10
+    W2[0, 2, 4] = np.inf
+    p = np.full((T, 1), 1.0, dtype=np.float32)
+    p[1:] = 0.9985
+    idx = np.zeros((T, 1), dtype=np.int32)
+    idx[2] = 1
+    got = _np(B.moe_experts(_to(x, dtype), _to(W13, dtype), _to(W2, dtype), _i32(idx), _to(p, "f32"), act="none"))
+    torch.cuda.synchronize()
+    big = np.float32(0.9985).astype(np.float64) * 2.0 ** 118
+    assert got[0, 0] == np.inf and got[0, 1] == -np.inf and got[0, 2] == np.inf
+    tol = (R.BF16 if dtype == "bf16" else 8 * R.U) * big
+    assert abs(got[1, 0] - big) <= tol and abs(got[1, 1] + big) <= tol and got[1, 2] == np.inf
+    assert abs(got[2, 0] + big) <= tol and abs(got[2, 1] - big) <= tol and abs(got[2, 2] + big) <= tol
