@@ -69,6 +69,12 @@ template <bool BF16> __device__ __forceinline__ f32x4 product(const u32x4& x, co
     }
 }
 
+// two bf16 numbers, 0 in place of an infinite one or NaN
+__device__ __forceinline__ uint32_t finite_halves(uint32_t v)
+{
+    return ((v & 0x7F80u) == 0x7F80u ? 0u : v & 0xFFFFu) | ((v & 0x7F800000u) == 0x7F800000u ? 0u : v & 0xFFFF0000u);
+}
+
 // the reference point of exponentials whose maximum is m: 0 where nothing was above -infinity
 __device__ __forceinline__ float origin(float m) { return m == -__builtin_inff() ? 0.0f : m; }
 
@@ -100,9 +106,10 @@ __global__ __launch_bounds__(ATT_THREADS, BF16 ? (VB == 1 && KS <= 4 ? 3 : 2) : 
     const long long lo = r.first + (long long)split * pl.chunk;
     const int begin = (int)lo, end = r.chunks == 0 ? begin : (int)(lo + pl.chunk < r.len ? lo + pl.chunk : r.len);
 
-    // queries: operand B, lane (m, g): head m, piece ks * 4 + g; zeros past Dk and past the group
-    const int h = hb * 16 + m;                   // of the group
+    const int h = hb * 16 + m;                   // the lane's head, of the group
     const long long hq = (long long)b * a.Hq + kvh * pl.G + h;
+
+    // queries: operand B, lane (m, g): head m, piece ks * 4 + g; zeros past Dk and past the group
     u32x4 qf[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
@@ -110,13 +117,6 @@ __global__ __launch_bounds__(ATT_THREADS, BF16 ? (VB == 1 && KS <= 4 ? 3 : 2) : 
         if (h < pl.G && (ks * 4 + g) * PER < a.c.Dk)
             qf[ks] = *(const u32x4*)((const unsigned char*)a.q + b * a.q_seq + (long long)(kvh * pl.G + h) * a.q_head + (ks * 4 + g) * 16);
     }
-
-    f32x4 o[VB][PER];
-    float top = -__builtin_inff(), sum = 0.0f;
-#pragma unroll
-    for (int vb = 0; vb < VB; ++vb)
-#pragma unroll
-        for (int j = 0; j < PER; ++j) o[vb][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     const long long part = ((long long)row * pl.S + split) * pl.G + h;
     const int heads_here = min(pl.G - hb * 16, 16);
@@ -127,206 +127,229 @@ __global__ __launch_bounds__(ATT_THREADS, BF16 ? (VB == 1 && KS <= 4 ? 3 : 2) : 
     const unsigned char* kbase = a.c.k + kvh * a.c.k_head;
     const unsigned char* vbase = a.c.v + kvh * a.c.v_head;
     const int slots = (1 << a.c.page_shift) - 1;
-    u32x4 kf[KS], vf[4][VB];
-    uint32_t live = 0;                           // which of the lane's 4 keys take part
+    // All of the chunk, its results written.  True where one of this thread's is not finite.  SPECIAL: values may be infinite or NaN.
+    auto run = [&](auto special_c) {
+        constexpr bool SPECIAL = decltype(special_c)::value;
+        f32x4 o[VB][PER];
+        float top = -__builtin_inff(), sum = 0.0f;
+#pragma unroll
+        for (int vb = 0; vb < VB; ++vb)
+#pragma unroll
+            for (int j = 0; j < PER; ++j) o[vb][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        u32x4 kf[KS], vf[4][VB];
+        uint32_t live = 0;                           // which of the lane's 4 keys take part
 
-    const long long stretch = (long long)TABLE << a.c.page_shift;        // positions whose page-table entries fit in LDS
-    for (long long p0 = begin; p0 < end; p0 += stretch) {
-        const int stop = p0 + stretch < end ? (int)(p0 + stretch) : end;
-        const int page0 = (int)p0 >> a.c.page_shift;
-        __syncthreads();
-        for (int i = threadIdx.x; i <= ((stop - 1) >> a.c.page_shift) - page0; i += ATT_THREADS)
-            lds.pages[i] = page_entry(a.c.table, a.c.max_pages, a.c.n_pages, b, page0 + i);
-        __syncthreads();
+        const long long stretch = (long long)TABLE << a.c.page_shift;        // positions whose page-table entries fit in LDS
+        for (long long p0 = begin; p0 < end; p0 += stretch) {
+            const int stop = p0 + stretch < end ? (int)(p0 + stretch) : end;
+            const int page0 = (int)p0 >> a.c.page_shift;
+            __syncthreads();
+            for (int i = threadIdx.x; i <= ((stop - 1) >> a.c.page_shift) - page0; i += ATT_THREADS)
+                lds.pages[i] = page_entry(a.c.table, a.c.max_pages, a.c.n_pages, b, page0 + i);
+            __syncthreads();
 
-        // Rows that do not take part (before the start, past the end, on no page) are read from the head's first row.  No
-        // branches: the entry is read at an index that is always in the table, and thrown away where the position is none.
-        const int last_entry = ((stop - 1) >> a.c.page_shift) - page0;
-        auto page_of = [&](int pos) {
-            const int i = (pos >> a.c.page_shift) - page0, page = lds.pages[min(max(i, 0), last_entry)];
-            return (int)(pos >= r.start) & (int)(pos < stop) & (int)(page >= 0) ? page : -1;
-        };
-        auto row_at = [&](const unsigned char* base, long long page_bytes, long long slot_bytes, int page, int pos) {
-            return base + max(page, 0) * page_bytes + (page < 0 ? 0 : pos & slots) * slot_bytes;
-        };
-        auto load_k = [&](int p) {
-            const unsigned char* at = row_at(kbase, a.c.k_page, a.c.k_slot, page_of(p + m), p + m);
+            // Rows that do not take part (before the start, past the end, on no page) are read from the head's first row.  No
+            // branches: the entry is read at an index that is always in the table, and thrown away where the position is none.
+            const int last_entry = ((stop - 1) >> a.c.page_shift) - page0;
+            auto page_of = [&](int pos) {
+                const int i = (pos >> a.c.page_shift) - page0, page = lds.pages[min(max(i, 0), last_entry)];
+                return (int)(pos >= r.start) & (int)(pos < stop) & (int)(page >= 0) ? page : -1;
+            };
+            auto row_at = [&](const unsigned char* base, long long page_bytes, long long slot_bytes, int page, int pos) {
+                return base + max(page, 0) * page_bytes + (page < 0 ? 0 : pos & slots) * slot_bytes;
+            };
+            auto load_k = [&](int p) {
+                const unsigned char* at = row_at(kbase, a.c.k_page, a.c.k_slot, page_of(p + m), p + m);
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const int piece = ks * 4 + g;
-                kf[ks] = *(const u32x4*)(at + (piece * PER < a.c.Dk ? piece : 0) * 16);
-            }
-        };
-        auto load_v = [&](int p) {
-            const int pos = p + g * 4;
-            int page[4];
-            if (a.c.page_shift >= 2) {           // four neighbours are on one page
-                const int i = (pos >> a.c.page_shift) - page0, one = lds.pages[min(max(i, 0), last_entry)];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) page[j] = (int)(pos + j >= r.start) & (int)(pos + j < stop) & (int)(one >= 0) ? one : -1;
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) page[j] = page_of(pos + j);
-            }
-            live = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const unsigned char* at = row_at(vbase, a.c.v_page, a.c.v_slot, page[j], pos + j);
-                live |= page[j] < 0 ? 0u : 1u << j;
-#pragma unroll
-                for (int vb = 0; vb < VB; ++vb) {
-                    const int piece = vb * 16 + m;
-                    vf[j][vb] = *(const u32x4*)(at + (piece * PER < a.c.Dv ? piece : 0) * 16);
+                for (int ks = 0; ks < KS; ++ks) {
+                    const int piece = ks * 4 + g;
+                    kf[ks] = *(const u32x4*)(at + (piece * PER < a.c.Dk ? piece : 0) * 16);
                 }
-            }
-        };
-
-        int p = (int)p0 + wave * TILE;
-        load_k(p);
-        load_v(p);
-        for (; p < stop; p += ATT_WAVES * TILE) {
-            if (a.c.Dk != KS * 4 * PER) {        // pieces past the key's end
+            };
+            auto load_v = [&](int p) {
+                const int pos = p + g * 4;
+                int page[4];
+                if (a.c.page_shift >= 2) {           // four neighbours are on one page
+                    const int i = (pos >> a.c.page_shift) - page0, one = lds.pages[min(max(i, 0), last_entry)];
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks)
+                    for (int j = 0; j < 4; ++j) page[j] = (int)(pos + j >= r.start) & (int)(pos + j < stop) & (int)(one >= 0) ? one : -1;
+                } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) kf[ks][i] = (ks * 4 + g) * PER < a.c.Dk ? kf[ks][i] : 0u;
-            }
-            f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+                    for (int j = 0; j < 4; ++j) page[j] = page_of(pos + j);
+                }
+                live = 0;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) s = product<BF16>(kf[ks], qf[ks], s);
-            const uint32_t now = live;
-            const int next = p + ATT_WAVES * TILE;
-            load_k(next);
-            __builtin_amdgcn_sched_barrier(0);   // requested here, not where they are used
-
-            if (!__all(now == 15u)) {
-                // what stands in a row that does not take part may be anything: no NaN of it may reach the sums
+                for (int j = 0; j < 4; ++j) {
+                    const unsigned char* at = row_at(vbase, a.c.v_page, a.c.v_slot, page[j], pos + j);
+                    live |= page[j] < 0 ? 0u : 1u << j;
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int vb = 0; vb < VB; ++vb)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) vf[j][vb][i] = (now >> j) & 1u ? vf[j][vb][i] : 0u;
-            }
-            float z[4], most = -__builtin_inff();
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                z[j] = (now >> j) & 1u ? s[j] * factor : -__builtin_inff();
-                most = fmaxf(most, z[j]);
-            }
-            if constexpr (MASS) {
-                // (a store without a branch, which the counting of outstanding loads would have to assume taken: what lies
-                // behind the head's row of the chunk, or past the group, is dropped by its offset)
-                const int at = p + g * 4 - begin;
-                __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(z[0]), __float_as_uint(z[1]), __float_as_uint(z[2]), __float_as_uint(z[3])},
-                                                       kept, at < pl.chunk ? (m * pl.chunk + at) * 4 : 0x7FFFFFF0, 0, 0);
-            }
-            most = fmaxf(most, __shfl_xor(most, 16, 64));
-            most = fmaxf(most, __shfl_xor(most, 32, 64));
-            if (__any(most > top)) {
-                const float higher = fmaxf(top, most), keep = exp2_(top - origin(higher));
-                top = higher;
-                sum *= keep;
-#pragma unroll
-                for (int vb = 0; vb < VB; ++vb)
-#pragma unroll
-                    for (int j = 0; j < PER; ++j)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) o[vb][j][i] *= keep;
-            }
-            const float at = origin(top);
-            float e[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                e[j] = exp2_(z[j] - at);
-                sum += e[j];
-            }
-            if constexpr (BF16) {
-                u32x2 part[3];                   // P: the nearest bf16 numbers, the nearest to what is left, and what then is left
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float left[2] = {e[2 * i], e[2 * i + 1]};
-#pragma unroll
-                    for (int u = 0; u < 3; ++u) {
-                        const uint32_t both = pack_bf16x2(left[0], left[1]);
-                        part[u][i] = both;
-                        left[0] -= __uint_as_float(both << 16);
-                        left[1] -= __uint_as_float(both & 0xFFFF0000u);
+                    for (int vb = 0; vb < VB; ++vb) {
+                        const int piece = vb * 16 + m;
+                        vf[j][vb] = *(const u32x4*)(at + (piece * PER < a.c.Dv ? piece : 0) * 16);
                     }
                 }
+            };
+
+            int p = (int)p0 + wave * TILE;
+            load_k(p);
+            load_v(p);
+            for (; p < stop; p += ATT_WAVES * TILE) {
+                if (a.c.Dk != KS * 4 * PER) {        // pieces past the key's end
 #pragma unroll
-                for (int vb = 0; vb < VB; ++vb)
+                    for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-                    for (int j = 0; j < PER; ++j) {
-                        u32x2 t;                 // dimension 8c + j of the lane's 4 keys
+                        for (int i = 0; i < 4; ++i) kf[ks][i] = (ks * 4 + g) * PER < a.c.Dk ? kf[ks][i] : 0u;
+                }
+                f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int i = 0; i < 2; ++i)
-                            t[i] = __builtin_amdgcn_perm(vf[2 * i + 1][vb][j >> 1], vf[2 * i][vb][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
-                        const short4v x = __builtin_bit_cast(short4v, t);
+                for (int ks = 0; ks < KS; ++ks) s = product<BF16>(kf[ks], qf[ks], s);
+                const uint32_t now = live;
+                const int next = p + ATT_WAVES * TILE;
+                load_k(next);
+                __builtin_amdgcn_sched_barrier(0);   // requested here, not where they are used
+
+                if (!__all(now == 15u)) {
+                    // what stands in a row that does not take part may be anything: no NaN of it may reach the sums
 #pragma unroll
-                        for (int u = 0; u < 3; ++u)
-                            o[vb][j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x, __builtin_bit_cast(short4v, part[u]), o[vb][j], 0, 0, 0);
-                    }
-            } else {
+                    for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                        for (int vb = 0; vb < VB; ++vb)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) vf[j][vb][i] = (now >> j) & 1u ? vf[j][vb][i] : 0u;
+                }
+                float z[4], most = -__builtin_inff();
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    z[j] = (now >> j) & 1u ? s[j] * factor : -__builtin_inff();
+                    most = fmaxf(most, z[j]);
+                }
+                if constexpr (MASS) {
+                    // (a store without a branch, which the counting of outstanding loads would have to assume taken: what lies
+                    // behind the head's row of the chunk, or past the group, is dropped by its offset)
+                    const int at = p + g * 4 - begin;
+                    __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(z[0]), __float_as_uint(z[1]), __float_as_uint(z[2]), __float_as_uint(z[3])},
+                                                           kept, at < pl.chunk ? (m * pl.chunk + at) * 4 : 0x7FFFFFF0, 0, 0);
+                }
+                most = fmaxf(most, __shfl_xor(most, 16, 64));
+                most = fmaxf(most, __shfl_xor(most, 32, 64));
+                if (__any(most > top)) {
+                    const float higher = fmaxf(top, most), keep = exp2_(top - origin(higher));
+                    top = higher;
+                    sum *= keep;
 #pragma unroll
                     for (int vb = 0; vb < VB; ++vb)
 #pragma unroll
                         for (int j = 0; j < PER; ++j)
-                            o[vb][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[i][vb][j]), e[i], o[vb][j], 0, 0, 0);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[vb][j][i] *= keep;
+                }
+                const float at = origin(top);
+                float e[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    e[j] = exp2_(z[j] - at);
+                    sum += e[j];
+                }
+                if constexpr (BF16) {
+                    u32x2 part[3];                   // P: the nearest bf16 numbers, the nearest to what is left, and what then is left
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float left[2] = {e[2 * i], e[2 * i + 1]};
+#pragma unroll
+                        for (int u = 0; u < 3; ++u) {
+                            const uint32_t both = pack_bf16x2(left[0], left[1]);
+                            part[u][i] = both;
+                            left[0] -= __uint_as_float(both << 16);
+                            left[1] -= __uint_as_float(both & 0xFFFF0000u);
+                        }
+                    }
+#pragma unroll
+                    for (int vb = 0; vb < VB; ++vb)
+#pragma unroll
+                        for (int j = 0; j < PER; ++j) {
+                            u32x2 t;                 // dimension 8c + j of the lane's 4 keys
+#pragma unroll
+                            for (int i = 0; i < 2; ++i)
+                                t[i] = __builtin_amdgcn_perm(vf[2 * i + 1][vb][j >> 1], vf[2 * i][vb][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+                            for (int u = 0; u < 3; ++u) {
+                                o[vb][j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(short4v, t), __builtin_bit_cast(short4v, part[u]), o[vb][j], 0, 0, 0);
+                                if (SPECIAL && u == 0)
+#pragma unroll
+                                    for (int i = 0; i < 2; ++i) t[i] = finite_halves(t[i]);
+                            }
+                        }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int vb = 0; vb < VB; ++vb)
+#pragma unroll
+                            for (int j = 0; j < PER; ++j)
+                                o[vb][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[i][vb][j]), e[i], o[vb][j], 0, 0, 0);
+                }
+                load_v(next);
+                asm volatile("" ::: "memory");       // here, not at the top of the next round
             }
-            load_v(next);
-            asm volatile("" ::: "memory");       // here, not at the top of the next round
         }
-    }
 
-    // the four waves' results: o[vb][j][i] of lane (m, g) is head m, dimension (vb * 16 + 4g + i) * PER + j.  They are added in
-    // LDS, wave w then writing the dimensions of i = w.
-    sum += __shfl_xor(sum, 16, 64);
-    sum += __shfl_xor(sum, 32, 64);
-    if (g == 0) {
-        wave_m[wave][m] = top;
-        wave_l[wave][m] = sum;
-    }
-    __syncthreads();
-    float all = wave_m[0][m], total = 0.0f;
-#pragma unroll
-    for (int w = 1; w < ATT_WAVES; ++w) all = fmaxf(all, wave_m[w][m]);
-#pragma unroll
-    for (int w = 0; w < ATT_WAVES; ++w) total += wave_l[w][m] * exp2_(wave_m[w][m] - origin(all));
-    const float mine = exp2_(top - origin(all));
-    const bool direct = r.chunks <= 1;
-    const float by = !direct ? 1.0f : total == 0.0f ? 0.0f : 1.0f / total;
-    if (wave == 0 && g == 0 && h < pl.G) {
-        if (!direct || MASS) pl.ml[part] = make_float2(all, total);
-        if (direct && a.lse) a.lse[hq] = (origin(all) + __log2f(total)) * LN2;
-    }
-#pragma unroll
-    for (int vb = 0; vb < VB; ++vb) {
-        if (vb > 0) __syncthreads();
-#pragma unroll
-        for (int j = 0; j < PER; ++j) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[vb][j][i] *= mine;
-            lds.o[wave][j][lane] = o[vb][j];
+        // the four waves' results: o[vb][j][i] of lane (m, g) is head m, dimension (vb * 16 + 4g + i) * PER + j.  They are added in
+        // LDS, wave w then writing the dimensions of i = w.
+        sum += __shfl_xor(sum, 16, 64);
+        sum += __shfl_xor(sum, 32, 64);
+        if (g == 0) {
+            wave_m[wave][m] = top;
+            wave_l[wave][m] = sum;
         }
         __syncthreads();
-        const int dim = (vb * 16 + 4 * g + wave) * PER;
-        if (h >= pl.G || dim >= a.c.Dv) continue;
-        float v[PER];
+        float all = wave_m[0][m], total = 0.0f;
 #pragma unroll
-        for (int j = 0; j < PER; ++j)
-            v[j] = ((lds.o[0][j][lane][wave] + lds.o[1][j][lane][wave]) + (lds.o[2][j][lane][wave] + lds.o[3][j][lane][wave])) * by;
-        if (BF16 && direct) {
-            *(u32x4*)((uint16_t*)a.out + hq * a.c.Dv + dim) =
-                u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[PER - 4], v[PER - 3]), pack_bf16x2(v[PER - 2], v[PER - 1])};
-        } else {
-            float* dst = direct ? (float*)a.out + hq * a.c.Dv + dim : pl.o + part * a.c.Dv + dim;
+        for (int w = 1; w < ATT_WAVES; ++w) all = fmaxf(all, wave_m[w][m]);
 #pragma unroll
-            for (int j = 0; j < PER; j += 4) *(f32x4*)(dst + j) = f32x4{v[j], v[j + 1], v[j + 2], v[j + 3]};
+        for (int w = 0; w < ATT_WAVES; ++w) total += wave_l[w][m] * exp2_(wave_m[w][m] - origin(all));
+        const float mine = exp2_(top - origin(all));
+        const bool direct = r.chunks <= 1;
+        const float by = direct ? 1.0f / total : 1.0f;
+        bool odd = false;
+        if (wave == 0 && g == 0 && h < pl.G) {
+            if (!direct || MASS) pl.ml[part] = make_float2(all, total);
+            if (direct && a.lse) a.lse[hq] = (origin(all) + __log2f(total)) * LN2;
         }
-    }
+#pragma unroll
+        for (int vb = 0; vb < VB; ++vb) {
+            if (vb > 0) __syncthreads();
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[vb][j][i] *= mine;
+                lds.o[wave][j][lane] = o[vb][j];
+            }
+            __syncthreads();
+            const int dim = (vb * 16 + 4 * g + wave) * PER;
+            if (h >= pl.G || dim >= a.c.Dv) continue;
+            float v[PER];
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                v[j] = ((lds.o[0][j][lane][wave] + lds.o[1][j][lane][wave]) + (lds.o[2][j][lane][wave] + lds.o[3][j][lane][wave])) * by;
+                v[j] = total == 0.0f ? 0.0f : v[j];          // no position, or none above -infinity
+                odd = odd || !__builtin_isfinite(v[j]);
+            }
+            if (BF16 && direct) {
+                *(u32x4*)((uint16_t*)a.out + hq * a.c.Dv + dim) =
+                    u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[PER - 4], v[PER - 3]), pack_bf16x2(v[PER - 2], v[PER - 1])};
+            } else {
+                float* dst = direct ? (float*)a.out + hq * a.c.Dv + dim : pl.o + part * a.c.Dv + dim;
+#pragma unroll
+                for (int j = 0; j < PER; j += 4) *(f32x4*)(dst + j) = f32x4{v[j], v[j + 1], v[j + 2], v[j + 3]};
+            }
+        }
+        return odd;
+    };
+    // An infinite value is right with the first part of P alone: a later one, 0 or below it, makes NaN of it.  So where a result
+    // is not finite the chunk is done again, with zeros for such values in the later products.
+    const bool odd = run(std::false_type{});
+    if constexpr (BF16)
+        if (__builtin_expect(__syncthreads_or(odd), 0)) run(std::true_type{});
 }
 
 static constexpr int JOIN_THREADS = 256, JOIN_WAVES = JOIN_THREADS / 64;

@@ -131,3 +131,74 @@ def test_moe_experts_with_infinite_hidden_values(T, dtype):
     tol = (R.BF16 if dtype == "bf16" else 8 * R.U) * big
     assert abs(got[1, 0] - big) <= tol and abs(got[1, 1] + big) <= tol and got[1, 2] == np.inf
     assert abs(got[2, 0] + big) <= tol and abs(got[2, 1] - big) <= tol and abs(got[2, 2] + big) <= tol
+
+
+def _attend_given(g, lengths, H, G, D, page, dtype, values, scale=None):
+    """attend and R.attend over random keys, the values being values(vp at the sequences' positions); masses too."""
+    kp, vp, table = _cache(g, lengths, H, D, D, page, dtype)
+    bad = vp.copy()
+    for b, n in enumerate(lengths):
+        p = np.arange(n)
+        rows = bad[table[b, p // page], :, p % page]              # [n, H, D]
+        bad[table[b, p // page], :, p % page] = values(b, rows)
+    q = _storage(g.standard_normal((len(lengths), H * G, D)), dtype)
+    mass = torch.zeros((len(lengths), H, table.shape[1] * page), device="cuda")
+    got = B.attend(_to(q, dtype), _pages(kp, dtype, "heads"), _pages(bad, dtype, "heads"), _i32(table), _i32(lengths), mass=mass,
+                   want_lse=True, scale=scale)
+    alone = B.attend(_to(q, dtype), _pages(kp, dtype, "heads"), _pages(bad, dtype, "heads"), _i32(table), _i32(lengths), scale=scale)
+    torch.cuda.synchronize()
+    assert torch.equal(got.out.nan_to_num(7.0), alone.out.nan_to_num(7.0))
+    return q, kp, vp, bad, table, got, _np(mass).astype(np.float64)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lengths", [[1, 2, 50], [200, 33, 17], [5000, 1], [3000, 900, 2049]])
+@pytest.mark.parametrize("H,G,D", [(1, 3, 64), (2, 17, 128), (1, 2, 256)])
+def test_attend_with_infinite_values(H, G, D, lengths, dtype):
+    """Infinite and NaN values at positions that are looked at: a dimension is what the formula gives; the others, and what
+    does not depend on the values, are as close as ever."""
+    def values(b, rows):
+        n = len(rows)
+        rows = rows.copy()
+        rows[0, 0, 3], rows[n - 1, 0, 9] = np.inf, -np.inf
+        rows[n // 2, 0, 20] = np.nan
+        rows[0, -1, 30] = -np.inf
+        if n > 1:
+            rows[0, -1, 40], rows[n - 1, -1, 40] = np.inf, -np.inf
+        rows[n // 3, -1, D - 1] = np.inf
+        return rows
+    q, kp, vp, bad, table, got, mass = _attend_given(np.random.default_rng(sum(lengths)), lengths, H, G, D, 16, dtype, values, scale=0.25 * D ** -0.5)
+    cap = table.shape[1] * 16
+    (out, lse, weight), tol = R.attend(q, kp, vp, table, lengths, None, 0.25 * D ** -0.5, cap, dtype == "bf16")
+    o = _np(got.out).astype(np.float64)
+    for b, n in enumerate(lengths):
+        for h in range(H):
+            p = np.arange(n)
+            rows = bad[table[b, p // 16], h, p % 16].astype(np.float64)
+            with np.errstate(invalid="ignore"):
+                special = rows[~np.isfinite(rows).all(1)].sum(0)                       # infinite or NaN as the weighted sum is
+            there = slice(h * G, (h + 1) * G)
+            odd = ~np.isfinite(special)
+            assert odd.any()
+            assert np.array_equal(o[b, there][:, odd], np.broadcast_to(special[odd], (G, odd.sum())), equal_nan=True)
+            assert (np.abs(o[b, there] - out[b, there]) <= tol[0][b, there])[:, ~odd].all()
+    assert (np.abs(_np(got.lse) - lse) <= tol[1]).all() and (np.abs(mass - weight) <= tol[2] + 2 * R.U * weight).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attend_is_zero_where_every_score_is_minus_infinity_whatever_the_values(dtype):
+    g = np.random.default_rng(44)
+    lengths = [9, 700, 300]
+    kp, vp, table = _cache(g, lengths, 1, 64, 64, 16, dtype)
+    kp[..., 0] = -np.inf
+    for b in range(2):
+        p = np.arange(lengths[b])
+        vp[table[b, p // 16], 0, p % 16] = [np.inf, -np.inf, np.nan, 1.0] * 16
+    p = np.arange(256, 300)                               # the last sequence: its first positions only
+    kp[table[2, p // 16], 0, p % 16, 0] = 0.0
+    q = np.abs(_storage(g.standard_normal((3, 2, 64)), dtype)) + 0.5
+    mass = torch.zeros((3, 1, 704), device="cuda")
+    got = B.attend(_to(q, dtype), _pages(kp, dtype, "heads"), _pages(vp, dtype, "heads"), _i32(table), _i32(lengths), mass=mass, want_lse=True)
+    torch.cuda.synchronize()
+    assert not _np(got.out)[:2].any() and np.isfinite(_np(got.out)[2]).all() and _np(got.out)[2].any()
+    assert (_np(got.lse)[:2] == -np.inf).all() and not _np(mass)[:2].any() and np.allclose(_np(mass)[2].sum(), 2.0, rtol=1e-5)
