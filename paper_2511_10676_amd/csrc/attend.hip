@@ -39,7 +39,7 @@ struct AttendPlan {
     int G, head_blocks;          // query heads of a key-value head, blocks of 16 of them
     int chunk, S;                // positions of a workgroup, chunks of the longest sequence
     int rows;                    // B * Hkv
-    float* o;                    // [rows][S][G][Dv] unnormalised outputs of the chunks (S > 1)
+    float* o;                    // [rows][S][G][Dv] outputs of the chunks, each over its own sum (S > 1)
     float2* ml;                  // [rows][S][G] their maxima (of scores in units of log2) and sums (S > 1 or mass)
     float* scores;               // [rows][S][G][chunk], in units of log2 (mass)
 };
@@ -127,9 +127,11 @@ __global__ __launch_bounds__(ATT_THREADS, BF16 ? (VB == 1 && KS <= 4 ? 3 : 2) : 
     const unsigned char* kbase = a.c.k + kvh * a.c.k_head;
     const unsigned char* vbase = a.c.v + kvh * a.c.v_head;
     const int slots = (1 << a.c.page_shift) - 1;
-    // All of the chunk, its results written.  True where one of this thread's is not finite.  SPECIAL: values may be infinite or NaN.
+    // All of the chunk, its results written.  True where one of this thread's is not finite.  SPECIAL: the values may be infinite or
+    // NaN, or near the largest number.
     auto run = [&](auto special_c) {
         constexpr bool SPECIAL = decltype(special_c)::value;
+        constexpr float unit = SPECIAL ? 0x1p-32f : 1.0f;    // what an exponential of 0 counts as
         f32x4 o[VB][PER];
         float top = -__builtin_inff(), sum = 0.0f;
 #pragma unroll
@@ -247,7 +249,7 @@ __global__ __launch_bounds__(ATT_THREADS, BF16 ? (VB == 1 && KS <= 4 ? 3 : 2) : 
                 float e[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    e[j] = exp2_(z[j] - at);
+                    e[j] = exp2_(z[j] - at) * unit;
                     sum += e[j];
                 }
                 if constexpr (BF16) {
@@ -309,11 +311,11 @@ __global__ __launch_bounds__(ATT_THREADS, BF16 ? (VB == 1 && KS <= 4 ? 3 : 2) : 
         for (int w = 0; w < ATT_WAVES; ++w) total += wave_l[w][m] * exp2_(wave_m[w][m] - origin(all));
         const float mine = exp2_(top - origin(all));
         const bool direct = r.chunks <= 1;
-        const float by = direct ? 1.0f / total : 1.0f;
+        const float by = 1.0f / total;
         bool odd = false;
         if (wave == 0 && g == 0 && h < pl.G) {
-            if (!direct || MASS) pl.ml[part] = make_float2(all, total);
-            if (direct && a.lse) a.lse[hq] = (origin(all) + __log2f(total)) * LN2;
+            if (!direct || MASS) pl.ml[part] = make_float2(all, total / unit);
+            if (direct && a.lse) a.lse[hq] = (origin(all) + __log2f(total / unit)) * LN2;
         }
 #pragma unroll
         for (int vb = 0; vb < VB; ++vb) {
@@ -346,10 +348,10 @@ __global__ __launch_bounds__(ATT_THREADS, BF16 ? (VB == 1 && KS <= 4 ? 3 : 2) : 
         return odd;
     };
     // An infinite value is right with the first part of P alone: a later one, 0 or below it, makes NaN of it.  So where a result
-    // is not finite the chunk is done again, with zeros for such values in the later products.
+    // is not finite the chunk is done again, with zeros for such values in the later products.  And the sum over up to 2^31 values
+    // may pass the largest number where their average does not: there its terms are 2^-32 of what they are.
     const bool odd = run(std::false_type{});
-    if constexpr (BF16)
-        if (__builtin_expect(__syncthreads_or(odd), 0)) run(std::true_type{});
+    if (__builtin_expect(__syncthreads_or(odd), 0)) run(std::true_type{});
 }
 
 static constexpr int JOIN_THREADS = 256, JOIN_WAVES = JOIN_THREADS / 64;
@@ -390,13 +392,16 @@ __global__ __launch_bounds__(JOIN_THREADS) void attend_join_kernel(AttendArgs a,
         if (r.chunks <= 1) return;                           // written already
         const long long part0 = ((long long)(b * a.c.Hkv + kvh) * pl.S) * pl.G + h;
         const float2 joined = join_chunks(pl.ml + part0, r.chunks, pl.G, lane);      // the same in every wave
-        const float at = origin(joined.x);
+        const float at = origin(joined.x), by = joined.y == 0.0f ? 0.0f : 1.0f / joined.y;
         // columns of 4 values; the threads of one column share the chunks
         const int cols = a.c.Dv / 4, groups = JOIN_THREADS / cols, col = tid % cols, grp = tid / cols;
         f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
         for (int s0 = 0; s0 < r.chunks; s0 += JOIN_THREADS) {
             if (s0 > 0) __syncthreads();
-            if (s0 + tid < r.chunks) weight[tid] = exp2_(pl.ml[part0 + (long long)(s0 + tid) * pl.G].x - at);
+            if (s0 + tid < r.chunks) {
+                const float2 c = pl.ml[part0 + (long long)(s0 + tid) * pl.G];
+                weight[tid] = exp2_(c.x - at) * c.y * by;
+            }
             __syncthreads();
             const int n = r.chunks - s0 < JOIN_THREADS ? r.chunks - s0 : JOIN_THREADS;
             if (grp < groups)
@@ -413,14 +418,11 @@ __global__ __launch_bounds__(JOIN_THREADS) void attend_join_kernel(AttendArgs a,
         const long long out = (long long)b * a.Hq + hq;
         if (tid == 0 && a.lse) a.lse[out] = (at + __log2f(joined.y)) * LN2;
         if (grp > 0) return;
-        const float by = joined.y == 0.0f ? 0.0f : 1.0f / joined.y;
         for (int q = 1; q < groups; ++q) {
             const f32x4 v = part_o[q * cols + col];
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[i] += v[i];
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] *= by;
         if constexpr (BF16) *(u32x2*)((uint16_t*)a.out + out * a.c.Dv + col * 4) = u32x2{pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3])};
         else *(f32x4*)((float*)a.out + out * a.c.Dv + col * 4) = acc;
     } else {

@@ -202,3 +202,21 @@ def test_attend_is_zero_where_every_score_is_minus_infinity_whatever_the_values(
     torch.cuda.synchronize()
     assert not _np(got.out)[:2].any() and np.isfinite(_np(got.out)[2]).all() and _np(got.out)[2].any()
     assert (_np(got.lse)[:2] == -np.inf).all() and not _np(mass)[:2].any() and np.allclose(_np(mass)[2].sum(), 2.0, rtol=1e-5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lengths,size", [([40, 1, 700], 3.2e38), ([9000], 3.2e38), ([4000], 1.5e36), ([2000, 1800], 4e36), ([300, 5], 1e37)])
+def test_attend_averages_values_near_the_largest_number(lengths, size, dtype):
+    """The sum of the values would overflow; their average, the result, does not (keys equal: the weights are 1 / n)."""
+    g = np.random.default_rng(50)
+    kp, vp, table = _cache(g, lengths, 2, 64, 64, 16, dtype)
+    kp[:], sign = 0.0, np.where(np.arange(64) % 3 == 0, -1.0, 1.0)
+    vp[:] = _storage(sign * size * (1.0 - np.arange(64) / 200.0), dtype)
+    q = _storage(g.standard_normal((len(lengths), 6, 64)), dtype)
+    got = B.attend(_to(q, dtype), _pages(kp, dtype, "heads"), _pages(vp, dtype, "heads"), _i32(table), _i32(lengths), want_lse=True)
+    torch.cuda.synchronize()
+    want = vp[0, 0, 0].astype(np.float64)
+    # a sum over n terms rounds n times at most, and so does the sum of the weights
+    tol = (2 * (np.array(lengths) + 16) * 2 * R.U + (R.BF16 if dtype == "bf16" else 0))[:, None, None] * np.abs(want)
+    assert (np.abs(_np(got.out).astype(np.float64) - want) <= tol).all()
+    assert np.allclose(_np(got.lse), np.log(lengths)[:, None], rtol=1e-5, atol=1e-6)
