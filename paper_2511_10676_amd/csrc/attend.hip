@@ -40,8 +40,8 @@ struct AttendPlan {
     int chunk, S;                // positions of a workgroup, chunks of the longest sequence
     int rows;                    // B * Hkv
     float* o;                    // [rows][S][G][Dv] outputs of the chunks, each over its own sum (S > 1)
-    float2* ml;                  // [rows][S][G] their maxima (of scores in units of log2) and sums (S > 1 or mass)
-    float* scores;               // [rows][S][G][chunk], in units of log2 (mass)
+    float2* ml;                  // [rows][S][G] the maxima of their scores, and their sums (S > 1 or mass)
+    float* scores;               // [rows][S][G][chunk] (mass)
 };
 
 // the part of a sequence that is looked at: positions start .. len, counted in chunks from start rounded down to a multiple of 16
@@ -56,7 +56,8 @@ __device__ __forceinline__ Range range_of(const int32_t* lengths, const int32_t*
     return r;
 }
 
-__device__ __forceinline__ float exp2_(float v) { return __builtin_amdgcn_exp2f(v); }
+// Of differences of scores only: a score in units of log2 may be past the largest number where the score itself is not.
+__device__ __forceinline__ float exp_(float v) { return __builtin_amdgcn_exp2f(v * LOG2E); }
 // 16 x 16 products of two operands of 16 rows x 64 bytes
 template <bool BF16> __device__ __forceinline__ f32x4 product(const u32x4& x, const u32x4& y, f32x4 acc)
 {
@@ -102,7 +103,6 @@ __global__ __launch_bounds__(ATT_THREADS, BF16 ? (VB == 1 && KS <= 4 ? 3 : 2) : 
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int m = lane & 15, g = lane >> 4;
-    const float factor = a.scale * LOG2E;
     const long long lo = r.first + (long long)split * pl.chunk;
     const int begin = (int)lo, end = r.chunks == 0 ? begin : (int)(lo + pl.chunk < r.len ? lo + pl.chunk : r.len);
 
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(ATT_THREADS, BF16 ? (VB == 1 && KS <= 4 ? 3 : 2) : 
                 float z[4], most = -__builtin_inff();
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    z[j] = (now >> j) & 1u ? s[j] * factor : -__builtin_inff();
+                    z[j] = (now >> j) & 1u ? s[j] * a.scale : -__builtin_inff();
                     most = fmaxf(most, z[j]);
                 }
                 if constexpr (MASS) {
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(ATT_THREADS, BF16 ? (VB == 1 && KS <= 4 ? 3 : 2) : 
                 most = fmaxf(most, __shfl_xor(most, 16, 64));
                 most = fmaxf(most, __shfl_xor(most, 32, 64));
                 if (__any(most > top)) {
-                    const float higher = fmaxf(top, most), keep = exp2_(top - origin(higher));
+                    const float higher = fmaxf(top, most), keep = exp_(top - origin(higher));
                     top = higher;
                     sum *= keep;
 #pragma unroll
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(ATT_THREADS, BF16 ? (VB == 1 && KS <= 4 ? 3 : 2) : 
                 float e[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    e[j] = exp2_(z[j] - at) * unit;
+                    e[j] = exp_(z[j] - at) * unit;
                     sum += e[j];
                 }
                 if constexpr (BF16) {
@@ -308,14 +308,14 @@ __global__ __launch_bounds__(ATT_THREADS, BF16 ? (VB == 1 && KS <= 4 ? 3 : 2) : 
 #pragma unroll
         for (int w = 1; w < ATT_WAVES; ++w) all = fmaxf(all, wave_m[w][m]);
 #pragma unroll
-        for (int w = 0; w < ATT_WAVES; ++w) total += wave_l[w][m] * exp2_(wave_m[w][m] - origin(all));
-        const float mine = exp2_(top - origin(all));
+        for (int w = 0; w < ATT_WAVES; ++w) total += wave_l[w][m] * exp_(wave_m[w][m] - origin(all));
+        const float mine = exp_(top - origin(all));
         const bool direct = r.chunks <= 1;
         const float by = 1.0f / total;
         bool odd = false;
         if (wave == 0 && g == 0 && h < pl.G) {
             if (!direct || MASS) pl.ml[part] = make_float2(all, total / unit);
-            if (direct && a.lse) a.lse[hq] = (origin(all) + __log2f(total / unit)) * LN2;
+            if (direct && a.lse) a.lse[hq] = origin(all) + __log2f(total / unit) * LN2;
         }
 #pragma unroll
         for (int vb = 0; vb < VB; ++vb) {
@@ -364,13 +364,13 @@ __device__ __forceinline__ float2 join_chunks(const float2* ml, int chunks, int 
     for (int s = lane; s < chunks; s += 64) {
         const float2 c = ml[(long long)s * G];
         const float higher = fmaxf(top, c.x);
-        total = total * exp2_(top - origin(higher)) + c.y * exp2_(c.x - origin(higher));
+        total = total * exp_(top - origin(higher)) + c.y * exp_(c.x - origin(higher));
         top = higher;
     }
 #pragma unroll
     for (int mask = 1; mask < 64; mask <<= 1) {
         const float ot = __shfl_xor(top, mask, 64), ol = __shfl_xor(total, mask, 64), higher = fmaxf(top, ot);
-        total = total * exp2_(top - origin(higher)) + ol * exp2_(ot - origin(higher));
+        total = total * exp_(top - origin(higher)) + ol * exp_(ot - origin(higher));
         top = higher;
     }
     // (two lanes may have rounded their sum of two products differently: everyone takes the first lane's)
@@ -400,7 +400,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void attend_join_kernel(AttendArgs a,
             if (s0 > 0) __syncthreads();
             if (s0 + tid < r.chunks) {
                 const float2 c = pl.ml[part0 + (long long)(s0 + tid) * pl.G];
-                weight[tid] = exp2_(c.x - at) * c.y * by;
+                weight[tid] = exp_(c.x - at) * c.y * by;
             }
             __syncthreads();
             const int n = r.chunks - s0 < JOIN_THREADS ? r.chunks - s0 : JOIN_THREADS;
@@ -416,7 +416,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void attend_join_kernel(AttendArgs a,
         part_o[tid] = acc;
         __syncthreads();
         const long long out = (long long)b * a.Hq + hq;
-        if (tid == 0 && a.lse) a.lse[out] = (at + __log2f(joined.y)) * LN2;
+        if (tid == 0 && a.lse) a.lse[out] = at + __log2f(joined.y) * LN2;
         if (grp > 0) return;
         for (int q = 1; q < groups; ++q) {
             const f32x4 v = part_o[q * cols + col];
@@ -460,7 +460,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void attend_join_kernel(AttendArgs a,
 #pragma unroll 4
             for (int h = 0; h < n; ++h)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) w[j] += exp2_(s[from[j] + (long long)h * pl.chunk] - head_m[h]) * head_by[h];
+                for (int j = 0; j < 4; ++j) w[j] += exp_(s[from[j] + (long long)h * pl.chunk] - head_m[h]) * head_by[h];
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j)

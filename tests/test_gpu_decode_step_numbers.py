@@ -220,3 +220,31 @@ def test_attend_averages_values_near_the_largest_number(lengths, size, dtype):
     tol = (2 * (np.array(lengths) + 16) * 2 * R.U + (R.BF16 if dtype == "bf16" else 0))[:, None, None] * np.abs(want)
     assert (np.abs(_np(got.out).astype(np.float64) - want) <= tol).all()
     assert np.allclose(_np(got.lse), np.log(lengths)[:, None], rtol=1e-5, atol=1e-6)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [7, 600])
+def test_attend_scores_near_the_largest_number(n, dtype):
+    """Finite scores up to 3.3e38 in size: equal ones share the weight, lower ones get none."""
+    kp, vp, table = _cache(np.random.default_rng(60), [n, n], 1, 64, 64, 16, dtype)
+    kp[:] = 0.0
+    vp[:] = _storage(np.random.default_rng(61).standard_normal(vp.shape), dtype)
+    q = np.zeros((2, 4, 64))
+    q[:, :, 0] = 1.0
+    big, less = _storage([3.3e38, 2.6e38], dtype)
+    kp[..., 0] = -big                                     # sequence 1: everywhere the lowest
+    p = np.arange(n)
+    kp[table[0, p // 16], 0, p % 16, 0] = less
+    kp[table[0, 1 // 16], 0, 1, 0] = kp[table[0, (n - 1) // 16], 0, (n - 1) % 16, 0] = big
+    mass = torch.zeros((2, 1, table.shape[1] * 16), device="cuda")
+    got = B.attend(_to(q, dtype), _pages(kp, dtype, "heads"), _pages(vp, dtype, "heads"), _i32(table), _i32([n, n]), scale=1.0, mass=mass, want_lse=True)
+    torch.cuda.synchronize()
+    rows = vp[table[:, p // 16], 0, p % 16].astype(np.float64)
+    want = np.stack([(rows[0, 1] + rows[0, n - 1]) / 2, rows[1].mean(0)])
+    tol = (n + 16) * 4 * R.U * np.abs(rows).max() + (R.BF16 if dtype == "bf16" else 0) * np.abs(want)
+    o = _np(got.out).astype(np.float64)
+    assert (np.abs(o - want[:, None]) <= tol[:, None]).all()
+    w = np.zeros((2, n))
+    w[0, [1, n - 1]], w[1] = 2.0, 4.0 / n
+    assert np.allclose(_np(mass)[:, 0, :n], w, rtol=1e-4, atol=0)
+    assert np.allclose(_np(got.lse)[0], big, rtol=1e-6) and np.allclose(_np(got.lse)[1], -big, rtol=1e-6)
