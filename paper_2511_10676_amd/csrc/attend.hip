@@ -504,7 +504,7 @@ bool attend_fits(const AttendArgs& a)
     if ((long long)a.c.B * a.c.Hkv >= (1ll << 23) || (long long)a.c.B * a.Hq >= (1ll << 23)) return false;
     const AttendPlan pl = plan_of(a);
     const long long wgs = ((long long)pl.rows * pl.S + 7) * pl.head_blocks;
-    const long long join = (long long)a.c.B * a.Hq + (long long)pl.rows * ((a.max_len + 15ll) / MASS_POSITIONS + 1);
+    const long long join = (long long)a.c.B * a.Hq + (a.mass ? (long long)pl.rows * ((a.max_len + 15ll) / MASS_POSITIONS + 1) : 0);
     return wgs < (1ll << 23) && join < (1ll << 23);              // a launch's threads stay below 2^32
 }
 
