@@ -402,7 +402,11 @@ typedef struct {
 } paep_attend_desc;
 
 /* Bytes of device workspace paep_attend needs for this shape, with or without
- * the mass output; 0 is possible, and the answer for an invalid descriptor. */
+ * the mass output; 0 is possible, and the answer for an invalid descriptor.
+ * The answer for a larger max_len or B is never less, so one workspace, asked for
+ * once for the cache's capacity, is enough for every step's own max_len.  With
+ * mass it holds a score per query head and position of max_len: about
+ * 4*B*Hq*max_len bytes. */
 size_t paep_attend_workspace_bytes(const paep_cache_desc *cache, const paep_attend_desc *desc, int32_t want_mass);
 
 /*

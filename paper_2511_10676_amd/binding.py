@@ -670,7 +670,8 @@ def attend(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_t
     v_pages [n_pages, Hkv, page_size, Dv], page_table [B, max_pages] int32, lengths [B] int32 -> out [B, Hq, Dv],
     lse [B, Hq] with want_lse.  A page that holds its slots outside its heads is passed as its transposed view.
     `scale` defaults to Dk ** -0.5; `starts` [B] int32: the first position each sequence looks at; `max_len`: a bound on
-    the lengths (default: what a row of the page table can hold) -- the work is laid out for it, so a tight one is faster;
+    the lengths (default: what a row of the page table can hold) -- the work is laid out for it, so a tight one is faster, and
+    with `mass` the workspace has 4 bytes for each of its positions at each query head;
     `mass` [B, Hkv, >= max_len] float32: increased by the attention weight of every position, summed over the query heads
     of its key-value head (what `cache_evict` goes by).  Sequences with nothing to look at give zeros."""
     with _on(stream):

@@ -476,22 +476,26 @@ __global__ __launch_bounds__(JOIN_THREADS) void attend_join_kernel(AttendArgs a,
 // sequences a chunk has at most 512 positions, because their lengths differ and the host does not know them (61 sequences of
 // 17 to 8192 positions with mass: 104 us, 116 in chunks of 2048; 61 of 1400 each 77 us, and 70 in one chunk each); one sequence
 // is cut into chunks of up to 2048.
+static constexpr int TARGET = 512, LEAST = 256;      // workgroups; positions of a chunk
+static constexpr int STEP = ATT_WAVES * TILE;        // positions that a workgroup's waves take at once
+// the most positions of a chunk: 2048, 512 where there are several sequences, and 1 / 256 of the longest where that is more
+static long long longest_chunk(const AttendArgs& a)
+{
+    const long long most = a.c.B > 1 ? 512 : 2048, share = (a.max_len + 255ll) / 256;
+    return most > share ? most : share;
+}
 static AttendPlan plan_of(const AttendArgs& a)
 {
-    constexpr int TARGET = 512, LEAST = 256;
     AttendPlan pl{};
     pl.G = a.Hq / a.c.Hkv;
     pl.head_blocks = (pl.G + 15) / 16;
     pl.rows = a.c.B * a.c.Hkv;
-    constexpr int step = ATT_WAVES * TILE;                       // positions that a workgroup's waves take at once
     const long long items = pl.rows > 0 ? (long long)pl.rows * pl.head_blocks : 1;
     long long chunk = ((long long)a.max_len * items + TARGET - 1) / TARGET;
-    long long most = a.c.B > 1 ? 512 : 2048;
-    if (most < (a.max_len + 255ll) / 256) most = (a.max_len + 255ll) / 256;     // 256 chunks of a sequence, for the join's sake
-    if (chunk > most) chunk = most;
+    if (chunk > longest_chunk(a)) chunk = longest_chunk(a);
     if (chunk < LEAST) chunk = LEAST;
     if (chunk > a.max_len + 16ll) chunk = a.max_len + 16ll;      // a first position is rounded down
-    pl.chunk = (int)((chunk + step - 1) / step * step);
+    pl.chunk = (int)((chunk + STEP - 1) / STEP * STEP);
     pl.S = (int)((a.max_len + 15ll + pl.chunk - 1) / pl.chunk);
     if (pl.S < 1) pl.S = 1;
     return pl;
@@ -508,15 +512,26 @@ bool attend_fits(const AttendArgs& a)
     return wgs < (1ll << 23) && join < (1ll << 23);              // a launch's threads stay below 2^32
 }
 
+// Enough for this call and for every one with a smaller max_len, B or Hkv (of the same G): the number of chunks falls where their
+// size grows by a step, so what is counted here are bounds that only grow.  For unrounded chunks of c positions,
+//   c >= LEAST                              chunks of all heads <= heads * ceil((max_len + 15) / LEAST)
+//   c = max_len * items / TARGET            <= TARGET * (query heads of an item) + 2 heads
+//   c = longest_chunk                       <= heads * ceil((max_len + 15) / c), and never more than 258 of a head
+// and a head's chunks have less than max_len + 15 + c positions together, c <= longest_chunk, max_len + 16, rounded to STEP.
 size_t attend_workspace_bytes(const AttendArgs& a)
 {
     const AttendPlan pl = plan_of(a);
-    const size_t parts = (size_t)a.c.B * a.Hq * pl.S;
+    const size_t heads = (size_t)a.c.B * a.Hq, positions = (size_t)a.max_len + 15;
+    auto least = [](size_t x, size_t y) { return x < y ? x : y; };
+    auto most = [](size_t x, size_t y) { return x > y ? x : y; };
+    auto chunks_of = [&](size_t c) { return (positions + c - 1) / c; };
+    const size_t parts = least(heads * chunks_of(LEAST), most(((size_t)TARGET * pl.G + pl.head_blocks - 1) / pl.head_blocks + 2 * heads,
+                                                              heads * least(chunks_of(a.c.B > 1 ? 512 : 2048), 258)));
     size_t n = 0;
-    if (pl.S > 1) n += up16(parts * a.c.Dv * 4);
-    if (pl.S > 1 || a.mass) n += up16(parts * 8);
-    if (a.mass) n += parts * pl.chunk * 4;
-    return n;
+    if (chunks_of(LEAST) > 1) n += up16(parts * a.c.Dv * 4);
+    if (chunks_of(LEAST) > 1 || a.mass) n += up16(parts * 8);
+    if (a.mass) n += heads * (positions + least(most(longest_chunk(a), LEAST), positions + 1) + STEP) * 4;
+    return heads ? n : 0;
 }
 
 template <bool BF16> static hipError_t launch(const AttendArgs& a, const AttendPlan& pl)

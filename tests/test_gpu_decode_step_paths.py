@@ -1,5 +1,7 @@
 """Paths of the decode step's operators that only some sizes take, against the 64-bit forms: workgroups of the expert layer that
 go on to further items, parts of rows added afterwards, every width of the selection, joins of several hundred chunks."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -64,3 +66,23 @@ def test_attend_walks_more_pages_than_a_workgroup_holds():
     table[0, 4444] = -1
     q = _storage(g.standard_normal((1, 2, D)), "bf16")
     _check_attend(q, kp, vp, table, [n], [3], "bf16")
+
+
+@pytest.mark.parametrize("mass", [False, True])
+@pytest.mark.parametrize("batch,H,G", [(1, 2, 4), (5, 1, 3), (61, 8, 1)])
+def test_attend_in_one_workspace_for_every_length(batch, H, G, mass):
+    """A workspace asked for once, for the table's capacity and the whole batch, is enough for tight bounds and parts of the batch."""
+    g = np.random.default_rng(batch)
+    page, width, D = 16, 130, 64
+    kp, vp, table = _cache(g, [width * page] * batch, H, D, D, page, "bf16")
+    q, kd, vd, td = _to(g.standard_normal((batch, H * G, D)), "bf16"), _pages(kp, "bf16", "heads"), _pages(vp, "bf16", "heads"), _i32(table)
+    c = B.CacheDesc(batch, H, D, D, page, kp.shape[0], width, B.BF16, H * page * D, page * D, D, H * page * D, page * D, D)
+    d = B.AttendDesc(H * G, width * page, 0.125, 0, H * G * D, D, width * page)
+    workspace = torch.empty(B.lib().paep_attend_workspace_bytes(ctypes.byref(c), ctypes.byref(d), mass), dtype=torch.uint8, device="cuda")
+    for n, few in ((1, batch), (241, batch), (242, 1), (260, batch), (272, batch), (400, (batch + 1) // 2), (1025, batch), (2080, batch)):
+        lengths = _i32([max(0, n - i) for i in range(few)])
+        sums = [torch.zeros((few, H, n), device="cuda") if mass else None for _ in range(2)]
+        got = B.attend(q[:few], kd, vd, td[:few], lengths, max_len=n, mass=sums[0], workspace=workspace)
+        want = B.attend(q[:few], kd, vd, td[:few], lengths, max_len=n, mass=sums[1])
+        torch.cuda.synchronize()
+        assert torch.equal(got.out, want.out) and (not mass or torch.equal(*sums))
