@@ -735,7 +735,7 @@ def cache_evict(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.
         _need_int32(dev, "out.lengths", out.lengths, (B,))
         _need_int32(dev, "out.kept", out.kept, (B, H, budget))
         _need_mass(dev, "out.mass", out.mass, B, H, min(budget, max_len))
-        if out.mass.data_ptr() == mass.data_ptr() or out.lengths.data_ptr() == lengths.data_ptr():
+        if B > 0 and (out.mass.data_ptr() == mass.data_ptr() or out.lengths.data_ptr() == lengths.data_ptr()):
             raise ValueError("out.mass and out.lengths must be other buffers than mass and lengths")
     st = lib().paep_cache_evict(c.desc, max_len, budget, recent, _ptr(k_pages), _ptr(v_pages), _ptr(page_table),
                                 _ptr(lengths), _ptr(mass), mass.shape[2], _ptr(out_table), out_table.shape[1], _ptr(out.kept),
