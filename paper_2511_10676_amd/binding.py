@@ -577,6 +577,12 @@ def _need_mass(dev: int, name: str, t: torch.Tensor, B: int, Hkv: int, least: in
         raise ValueError(f"{name} must be contiguous float32 [{B}, {Hkv}, at least {least}] on the cache's device")
 
 
+def _need_32_bits(name: str, v: int) -> None:
+    """The library's integers have 32 bits, and what does not fit would be cut off on the way there."""
+    if not -1 << 31 <= v < 1 << 31:
+        raise ValueError(f"{name} must fit in 32 bits")
+
+
 def _stride(t: torch.Tensor, dim: int) -> int:
     """Stride of a dimension; 0 where it has one entry (torch leaves any value there)."""
     return t.stride(dim) if t.shape[dim] > 1 else 0
@@ -589,7 +595,7 @@ class _Cache(NamedTuple):
     Hkv: int
     Dk: int
     Dv: int
-    capacity: int             # positions of a page-table row
+    capacity: int             # positions of a page-table row, or as many as the library counts
 
 
 def _cache(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor) -> _Cache:
@@ -614,7 +620,8 @@ def _cache(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tenso
     if ps < 2:
         ks = vs = 0
     Dv = v_pages.shape[3]
-    return _Cache(_CACHE_BYTES.pack(B, H, Dk, Dv, ps, n, width, dt, kp, kh, ks, vp, vh, vs), dev, B, H, Dk, Dv, width * ps)
+    return _Cache(_CACHE_BYTES.pack(B, H, Dk, Dv, ps, n, width, dt, kp, kh, ks, vp, vh, vs), dev, B, H, Dk, Dv,
+                  min(width * ps, 0x7FFF0000))
 
 
 class Attention(NamedTuple):
@@ -638,6 +645,8 @@ def prepare_attend(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor
         _need_int32(dev, "starts", starts, (B,))
     if max_len is None:
         max_len = c.capacity
+    else:
+        _need_32_bits("max_len", max_len)
     if mass is not None:
         _need_mass(dev, "mass", mass, B, c.Hkv, max_len)
     if out is None:
@@ -670,8 +679,8 @@ def attend(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_t
     v_pages [n_pages, Hkv, page_size, Dv], page_table [B, max_pages] int32, lengths [B] int32 -> out [B, Hq, Dv],
     lse [B, Hq] with want_lse.  A page that holds its slots outside its heads is passed as its transposed view.
     `scale` defaults to Dk ** -0.5; `starts` [B] int32: the first position each sequence looks at; `max_len`: a bound on
-    the lengths (default: what a row of the page table can hold) -- the work is laid out for it, so a tight one is faster, and
-    with `mass` the workspace has 4 bytes for each of its positions at each query head;
+    the lengths (default: what a row of the page table can hold, 2^31 - 2^16 at most) -- the work is laid out for it, so a
+    tight one is faster, and with `mass` the workspace has 4 bytes for each of its positions at each query head;
     `mass` [B, Hkv, >= max_len] float32: increased by the attention weight of every position, summed over the query heads
     of its key-value head (what `cache_evict` goes by).  Sequences with nothing to look at give zeros."""
     with _on(stream):
@@ -721,6 +730,8 @@ def cache_evict(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.
     dev, B, H = c.dev, c.B, c.Hkv
     if max_len is None:
         max_len = c.capacity
+    else:
+        _need_32_bits("max_len", max_len)
     _need_mass(dev, "mass", mass, B, H, max_len)
     if out_table.dim() != 2 or out_table.shape[0] != B:
         raise ValueError("out_table must be [B, out_pages]")
@@ -728,6 +739,8 @@ def cache_evict(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.
     _need_int32(dev, "out_table", out_table, None)
     if budget < 1:
         raise ValueError("budget must be at least 1")
+    _need_32_bits("budget", budget)
+    _need_32_bits("recent", recent)
     if out is None:
         with _on(stream):
             out = Eviction(torch.empty_like(lengths), lengths.new_empty((B, H, budget)), torch.empty_like(mass))
@@ -767,6 +780,7 @@ def _prepare_moe(x, W13, W2, k, act, prob, residual, y, workspace):
     for t in (residual, y):
         if t is not None and t.shape != x.shape:
             raise ValueError("residual and y must be [T, d]")
+    _need_32_bits("k", k)
     desc = MoeDesc(T, d, f, E, k, dt, ACT[act], PROB[prob])
     if y is None:
         y = torch.empty_like(x)
