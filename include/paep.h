@@ -491,7 +491,7 @@ typedef struct {
 
 #define PAEP_MOE_MAX_T 64
 
-/* Bytes of device workspace that paep_moe_layer and paep_moe_experts need; 0 for an invalid descriptor. */
+/* Bytes of device workspace that paep_moe_layer and paep_moe_experts need, for more tokens never less; 0 for an invalid descriptor. */
 size_t paep_moe_workspace_bytes(const paep_moe_desc *desc);
 
 /*

@@ -18,12 +18,14 @@
 // sums that cancel had fewer right bits than its storage, and the third instruction costs nothing next to the loads (the
 // cases below: 0.2 % at most).
 // The next tile's keys are requested once this tile's are multiplied, the next values likewise, so that a wave always has a
-// tile in flight.  Tiles of 16 positions, not of 32, leave registers for three workgroups on a CU instead of two (131071
-// positions 58 -> 56 us, 32 heads on one key-value head of width 256 56 -> 48 us), and one block of 16 query heads to a
-// workgroup, not two, for two (32 heads of width 256 94 -> 55 us, of width 128 32 -> 25 us).  Waves are joined in LDS, chunks by
+// tile in flight.  Tiles of 16 positions, not of 32, leave registers for three workgroups on a CU instead of two (when taken,
+// 131071 positions 58 -> 56 us, 32 heads on one key-value head of width 256 56 -> 48 us), and one block of 16 query heads to a
+// workgroup, not two, for two (likewise, 32 heads of width 256 94 -> 55 us, of width 128 32 -> 25 us).  Waves are joined in LDS, chunks by
 // attend_join_kernel, in a fixed order.
-// Measured: 131071 positions of 4 key-value heads of 128 56 us (4.7 TB/s, 5.3 without the join's launch); 61 sequences of
-// 17 to 8192 positions, 8 heads, with mass 104 us.
+// A chunk whose results are not all finite is done a second time, in a form for infinite values and sums past the largest
+// number; looking whether they are costs 0.4 us of a call.
+// Measured: 131071 positions of 4 key-value heads of 128 57 us (4.7 TB/s, 5.2 without the join's launch); 61 sequences of
+// 17 to 8192 positions, 8 heads, with mass 104 us; fp32, 5 sequences of up to 4096 positions, 3 heads of 80, 18 us.
 #include <type_traits>
 
 #include "cache_device.h"
@@ -472,10 +474,10 @@ __global__ __launch_bounds__(JOIN_THREADS) void attend_join_kernel(AttendArgs a,
 
 // How the positions are cut.  The longest sequences are cut into enough chunks that there are two workgroups for every CU, if
 // a chunk then still has 256 positions (four tiles per wave): a smaller one costs a join that takes longer than it saves (one
-// sequence of 151 positions 8.1 us whole, 10.8 in two chunks; 131071 positions 56 us, for three workgroups per CU 61).  With several
+// sequence of 151 positions 8.5 us whole, 11.3 in two chunks; 131071 positions 58 us, for three workgroups per CU 63).  With several
 // sequences a chunk has at most 512 positions, because their lengths differ and the host does not know them (61 sequences of
-// 17 to 8192 positions with mass: 104 us, 116 in chunks of 2048; 61 of 1400 each 77 us, and 70 in one chunk each); one sequence
-// is cut into chunks of up to 2048.
+// 17 to 8192 positions with mass: 105 us, 129 in chunks of 2048; where the lengths are equal it costs: 61 of 1400 each 80 us, and
+// 66 in one chunk each); one sequence is cut into chunks of up to 2048.
 static constexpr int TARGET = 512, LEAST = 256;      // workgroups; positions of a chunk
 static constexpr int STEP = ATT_WAVES * TILE;        // positions that a workgroup's waves take at once
 // the most positions of a chunk: 2048, 512 where there are several sequences, and 1 / 256 of the longest where that is more

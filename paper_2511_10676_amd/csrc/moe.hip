@@ -12,14 +12,15 @@
 //                   four waves split d.  h goes to the workspace in fp32, already weighed by p
 //   down_kernel     16 rows of d over all active experts: the eight waves split (expert, part of f); sums per token in LDS.
 //                   With h in 16 bits (two bf16 parts, stored) sums that cancel had fewer right bits than y can hold; taking all
-//                   24 bits of it apart here costs 1 to 3 % of the layer
+//                   24 bits of it apart here costs 1.5 to 4 us of the layer
 //   sum_kernel      where two or more workgroups share 16 rows
 // A fragment of 16 rows x 64 bytes is fetched with four neighbouring lanes on 64 contiguous bytes of a row, and a fixed lane
 // permutation puts it into the operand layout (as in predict_decode.hip).
-// Measured (us; up / down kernel): 61 tokens, 64 experts 2048 x 1408, top 6: 230 (134 at 5.5 TB/s / 73 at 5.1); 16 tokens, 16
-// experts 4096 x 960, top 2: 80 (43 / 23); one token, 8 experts 2048 x 768: 31 (12 / 9, the other two launches 10); fp32, 7
-// tokens, 32 experts 1024 x 704, top 4: 53 (25 / 15).  With a list per workgroup, d = 2048 in 128 workgroups and masks
-// applied behind the loads, which are then waited for at once: 356, 91, 38, 87.
+// Measured (us; up / down kernel): 61 tokens, 64 experts 2048 x 1408, top 6: 233 (130 at 5.7 TB/s / 79 at 4.7); 16 tokens, 16
+// experts 4096 x 960, top 2: 82 (43 / 26); one token, 8 experts 2048 x 768: 33 (13 / 11, the other two launches 10); fp32, 7
+// tokens, 32 experts 1024 x 704, top 4: 52 (25 / 15); 64 tokens, 16 experts 4096 x 960, top 2: 99; 64 tokens, 8 experts
+// 2048 x 768, top 4, 32 tokens to each: 61.  (The first form, with a list per workgroup, d = 2048 in 128 workgroups and masks
+// applied behind the loads, which are then waited for at once, took 356, 91, 38 and 87 for the first four.)
 #include <type_traits>
 
 #include "../../include/paep.h"
@@ -572,8 +573,8 @@ static size_t h_bytes(const MoeArgs& a) { return ((size_t)a.T * a.k * a.f * 4 + 
 
 static size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 // Workgroups that share 16 rows of d: enough for one per CU (a workgroup's registers leave room for no second), unless a wave would
-// have fewer than 64 steps -- the sums' launch then costs what the other CUs gain (one token, 8 experts of 2048 x 768: 31 us
-// both ways; 61 tokens of 64 experts 243 us in two parts, 302 in one; more parts than CUs: 265).
+// have fewer than 64 steps -- the sums' launch then costs most of what the other CUs gain (one token, 8 experts of 2048 x 768:
+// 32.7 us, in two parts 31.9; 61 tokens of 64 experts 233 us in two parts, 282 in one, 240 in four).
 static int down_parts(const MoeArgs& a)
 {
     const int tiles = (a.d + 15) / 16, parts = (256 + tiles - 1) / tiles;
