@@ -5,9 +5,9 @@ A case is one pass through one of these:
 * ``rotate``   the position rotation of the queries and keys of some tokens, behind a norm of each head;
 * ``place``    the same with the keys and values going into the pages of a cache (``rotate_append``);
 * ``append4``  keys and values rounded to 4 bits into the pages of a cache, and what then stands there read back
-               (``cache_append_fp4``, ``cache_read_fp4``);
-* ``read4``    a stretch of such a cache read back (``cache_read_fp4``);
-* ``attend4``  attention of one new token per sequence over such a cache (``attend_fp4``).
+               (``cache_append_fourbit``, ``cache_read_fourbit``);
+* ``read4``    a stretch of such a cache read back (``cache_read_fourbit``);
+* ``attend4``  attention of one new token per sequence over such a cache (``attend_fourbit``).
 
 Four bits: 32 neighbours of a row share a power of two, 2^(byte - 127), and each is a sign and one of the magnitudes
 0, 0.5, 1, 1.5, 2, 3, 4, 6; the even neighbour stands in a byte's lower half.  The power is the smallest with which none
@@ -300,11 +300,11 @@ def _run_own(s):
                             style=case["style"], q_weight=s["q_weight"], k_weight=s["k_weight"], eps=EPS)
         return [q, s["k_pages"], s["v_pages"]]
     if case["kind"] == "attend4":
-        got = B.attend_fp4(s["q"], *cache, s["lengths"], starts=s["starts"], max_len=s["cap"], want_lse=case["lse"])
+        got = B.attend_fourbit(s["q"], *cache, s["lengths"], starts=s["starts"], max_len=s["cap"], want_lse=case["lse"])
         return [x for x in (got.out, got.lse) if x is not None]
     if case["kind"] == "append4":
-        B.cache_append_fp4(s["k"], s["v"], *cache, s["pos"], sequences=s["seq"])
-    got = B.cache_read_fp4(*cache, s["pos"], sequences=s["seq"], dtype=DTYPE[case["dtype"]])
+        B.cache_append_fourbit(s["k"], s["v"], *cache, s["pos"], sequences=s["seq"])
+    got = B.cache_read_fourbit(*cache, s["pos"], sequences=s["seq"], dtype=DTYPE[case["dtype"]])
     return [got.k, got.v]
 
 
