@@ -11,8 +11,9 @@
  * at once, the per-expert grouping of its selections (the prefetch list), and
  * the accuracy counters of section 5.1.  Beside it stands what the same layer
  * runs in a decode step while its experts are fetched and once they are there:
- * attention of one new token over a paged key-value cache, the cache's upkeep,
- * and the mixture-of-experts layer itself.
+ * the rotation of queries and keys by position, attention of one new token over
+ * a paged key-value cache (in 16, 32 or 4 bits), the cache's upkeep, and the
+ * mixture-of-experts layer itself.
  *
  * Conventions for every entry point
  *   - Pointers named *_dev are DEVICE pointers owned by the caller (inputs,
@@ -476,6 +477,118 @@ paep_status paep_cache_evict(const paep_cache_desc *cache, int32_t max_len, int3
                              const int32_t *out_table_dev, int32_t out_max_pages,
                              int32_t *kept_dev, float *mass_out_dev, int64_t mass_out_stride, int32_t *lengths_out_dev,
                              void *stream);
+
+/* Which dimensions of a head turn together: i and i + rot/2, or 2i and 2i + 1. */
+typedef enum { PAEP_ROTATE_HALVES = 0, PAEP_ROTATE_PAIRS = 1 } paep_rotate_style;
+
+/* The queries and keys of n tokens, on their way from a projection to attention. */
+typedef struct {
+    int32_t n;              /* tokens, 0..2^24 */
+    int32_t Hq;             /* query heads, 0..PAEP_MAX_HEADS */
+    int32_t Hk;             /* key heads, 0..PAEP_MAX_HEADS; one of the two above 0 */
+    int32_t D;              /* width of a head, multiple of 8, 8..PAEP_MAX_HEAD_DIM */
+    int32_t rot;            /* dimensions that are rotated, the first ones: even, 2..D */
+    int32_t table_rows;     /* positions in the table, >= 1 */
+    int32_t dtype;          /* paep_dtype of q, k, v, the weights and the outputs */
+    int32_t style;          /* paep_rotate_style */
+    float eps;              /* of the norms, finite, > 0 */
+    int32_t reserved;       /* 0 */
+    int64_t q_row_stride, q_head_stride;            /* elements between two tokens, two heads: inputs ... */
+    int64_t k_row_stride, k_head_stride;
+    int64_t q_out_row_stride, q_out_head_stride;    /* ... and outputs; all 16-byte aligned */
+    int64_t k_out_row_stride, k_out_head_stride;    /* (paep_rotate alone) */
+} paep_rotate_desc;
+
+/*
+ * Norm of each head and rotation by position, in one pass, for every head of
+ * q (weight w = q_weight) and k (k_weight):
+ *     x' = w x / sqrt(mean of x^2 over the head + eps)   where there is a weight, else x
+ *     (y_a, y_b) = (x'_a cos - x'_b sin, x'_a sin + x'_b cos)   for pair i of rot/2,
+ *         a, b = i, i + rot/2 or 2i, 2i + 1 as style says,
+ *         cos = table[positions[t]][i],  sin = table[positions[t]][rot/2 + i]
+ *     y = x' in the other dimensions
+ * fp32, rounded once.  A token whose position is outside [0, table_rows) is left
+ * out: its outputs stay as they were.
+ *   q_dev, k_dev [n] rows of Hq, Hk heads of D (a NULL where there are no heads)
+ *   q_weight_dev, k_weight_dev [D] or NULL;  positions_dev [n] int32
+ *   table_dev [table_rows][rot] float
+ *   q_out_dev, k_out_dev: may be q_dev and k_dev with the same strides, else
+ *       they overlap no input
+ * Pointers but positions_dev must be 16-byte aligned.
+ */
+paep_status paep_rotate(const paep_rotate_desc *desc, const void *q_dev, const void *k_dev,
+                        const void *q_weight_dev, const void *k_weight_dev, const int32_t *positions_dev,
+                        const float *table_dev, void *q_out_dev, void *k_out_dev, void *stream);
+
+/*
+ * The same with the keys, and the values, going into a cache (of Hkv = Hk,
+ * Dk = D and the same dtype; k_out strides are not looked at): those of token i
+ * to position positions[i] of sequence sequences[i], as in paep_cache_append,
+ * which also says which rows are skipped.  (A query is rotated wherever its
+ * key goes.)  angles_dev [n] int32 or NULL: the rows of the table, where they
+ * are not the positions, as after paep_cache_evict.  A token at no row of the
+ * table is left out, its key and value too.
+ *   v_dev [n] rows of Hk heads of Dv, strides 16-byte aligned
+ *   mass_dev as in paep_cache_append
+ */
+paep_status paep_rotate_append(const paep_rotate_desc *desc, const paep_cache_desc *cache, const void *q_dev,
+                               const void *k_dev, const void *v_dev, int64_t v_row_stride, int64_t v_head_stride,
+                               const void *q_weight_dev, const void *k_weight_dev, const float *table_dev,
+                               const int32_t *angles_dev, void *q_out_dev, void *k_pages_dev, void *v_pages_dev,
+                               const int32_t *page_table_dev, const int32_t *sequences_dev, const int32_t *positions_dev,
+                               float *mass_dev, int64_t mass_stride, void *stream);
+
+/*
+ * ---- a cache in 4 bits ----
+ *
+ * 32 neighbours of a key or value, a group, share a byte, the power of two
+ * 2^(byte - 127).  Each of them is a code of 4 bits times that power: a sign
+ * (bit 3) and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0 to 7).  Two codes to a
+ * byte, the lower half the first, so a row of Dk elements has Dk/2 bytes.
+ *   - The pools hold the codes; a paep_cache_desc describes them with Dk and Dv
+ *     multiples of 32, strides in ELEMENTS, multiples of 32, and dtype that of
+ *     the queries, new keys and values and outputs.
+ *   - k_scales_dev is [n_pages][Hkv][Dk/32][page_size] uint8, dense: neighbours
+ *     in position are neighbours in memory.  v_scales_dev likewise.
+ * Bytes are 2..252, with which every number of a group is 0 or a normal fp32
+ * and bf16 number, or 255: all 32 are NaN.  (No call checks them; others give
+ * numbers that are not fixed here.)  Pools and scales must be 16-byte aligned.
+ * Everything else as for a cache of dtype.
+ */
+
+/*
+ * paep_cache_append into a cache in 4 bits.  A group's power is the smallest
+ * of 2^-125..2^125 with which its largest magnitude is at most 7 powers; every
+ * element becomes the nearest number, of two equally near the one of even
+ * code, an infinite one the largest.  So none is off by more than half a step
+ * where it lands, but for what is past 7 * 2^125.  A group with NaN is NaN.
+ *   k_dev [n] rows of Hkv keys, strides in elements, 16-byte aligned; v_dev likewise
+ */
+paep_status paep_cache_append_fourbit(const paep_cache_desc *cache, int32_t n, const void *k_dev, int64_t k_row_stride,
+                                  int64_t k_head_stride, const void *v_dev, int64_t v_row_stride, int64_t v_head_stride,
+                                  void *k_pages_dev, void *v_pages_dev, uint8_t *k_scales_dev, uint8_t *v_scales_dev,
+                                  const int32_t *page_table_dev, const int32_t *sequences_dev, const int32_t *positions_dev,
+                                  void *stream);
+
+/*
+ * The way back: row i of k_out_dev [n][Hkv][Dk] and v_out_dev [n][Hkv][Dv] is
+ * what stands at position positions[i] of sequence sequences[i] (of sequence i
+ * where sequences_dev is NULL; n <= B then), exactly; zeros where that names no
+ * place.  The same place may be named several times.
+ */
+paep_status paep_cache_read_fourbit(const paep_cache_desc *cache, int32_t n, const void *k_pages_dev, const void *v_pages_dev,
+                                const uint8_t *k_scales_dev, const uint8_t *v_scales_dev, const int32_t *page_table_dev,
+                                const int32_t *sequences_dev, const int32_t *positions_dev, void *k_out_dev, void *v_out_dev,
+                                void *stream);
+
+/* paep_attend over a cache in 4 bits, without the mass output (mass_stride is
+ * not looked at). */
+size_t paep_attend_fourbit_workspace_bytes(const paep_cache_desc *cache, const paep_attend_desc *desc);
+paep_status paep_attend_fourbit(const paep_cache_desc *cache, const paep_attend_desc *desc, const void *q_dev,
+                            const void *k_pages_dev, const void *v_pages_dev, const uint8_t *k_scales_dev,
+                            const uint8_t *v_scales_dev, const int32_t *page_table_dev, const int32_t *lengths_dev,
+                            const int32_t *starts_dev, void *out_dev, float *lse_dev,
+                            void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /* Shape of a mixture-of-experts layer for a few tokens. */
 typedef struct {

@@ -24,6 +24,7 @@ F32, BF16 = 0, 1
 ACT = {"none": 0, "silu": 1, "gelu": 2}
 PATH = {"auto": 0, "simple": 1, "decode": 2, "prefill": 3}
 PATH_NAME = {v: k for k, v in PATH.items()}
+ROTATE_STYLE = {"halves": 0, "pairs": 1}
 PROB = {"softmax": 0, "softmax_topk": 1, "sigmoid": 2}
 TILE_CFG = {0: "128x128", 1: "128x128 wide", 2: "256x256", 3: "256x128", 4: "256x256 wide", 5: "64x64",
             6: "two-pass 256x256", 7: "128-256x256"}
@@ -42,7 +43,9 @@ EXPORTS = ["paep_predict_workspace_bytes", "paep_predict_workspace_min_bytes", "
            "paep_score_rows", "paep_confidence_select", "paep_activation_profile", "paep_probe_read",
            "paep_probe_mfma", "paep_status_string", "paep_version",
            "paep_attend_workspace_bytes", "paep_attend", "paep_cache_append", "paep_cache_evict",
-           "paep_moe_workspace_bytes", "paep_moe_layer", "paep_moe_experts"]
+           "paep_moe_workspace_bytes", "paep_moe_layer", "paep_moe_experts",
+           "paep_rotate", "paep_rotate_append", "paep_cache_append_fourbit", "paep_cache_read_fourbit",
+           "paep_attend_fourbit_workspace_bytes", "paep_attend_fourbit"]
 
 
 class PredictDesc(ctypes.Structure):
@@ -60,13 +63,20 @@ class CacheDesc(ctypes.Structure):
                                               "v_page_stride", "v_head_stride", "v_slot_stride")]
 
 
-# the same bytes as the two structures, in a third of the time
-_CACHE_BYTES, _ATTEND_BYTES = struct.Struct("8i6q"), struct.Struct("2ifi3q")
+# the same bytes as the structures, in a third of the time
+_CACHE_BYTES, _ATTEND_BYTES, _ROTATE_BYTES = struct.Struct("8i6q"), struct.Struct("2ifi3q"), struct.Struct("8ifi8q")
 
 
 class AttendDesc(ctypes.Structure):
     _fields_ = [("Hq", ctypes.c_int32), ("max_len", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
                 ("q_seq_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64), ("mass_stride", ctypes.c_int64)]
+
+
+class RotateDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n", "Hq", "Hk", "D", "rot", "table_rows", "dtype", "style")] + \
+               [("eps", ctypes.c_float), ("reserved", ctypes.c_int32)] + \
+               [(n, ctypes.c_int64) for n in ("q_row_stride", "q_head_stride", "k_row_stride", "k_head_stride",
+                                              "q_out_row_stride", "q_out_head_stride", "k_out_row_stride", "k_out_head_stride")]
 
 
 class MoeDesc(ctypes.Structure):
@@ -145,6 +155,18 @@ def lib() -> ctypes.CDLL:
         L.paep_cache_append.restype = ctypes.c_int
         L.paep_cache_evict.argtypes = [cp, i32, i32, i32] + [vp] * 5 + [i64, vp, i32, vp, vp, i64, vp, vp]
         L.paep_cache_evict.restype = ctypes.c_int
+        L.paep_rotate.argtypes = [vp] * 10
+        L.paep_rotate.restype = ctypes.c_int
+        L.paep_rotate_append.argtypes = [vp, cp, vp, vp, vp, i64, i64] + [vp] * 11 + [i64, vp]
+        L.paep_rotate_append.restype = ctypes.c_int
+        L.paep_cache_append_fourbit.argtypes = [cp, i32, vp, i64, i64, vp, i64, i64] + [vp] * 8
+        L.paep_cache_append_fourbit.restype = ctypes.c_int
+        L.paep_cache_read_fourbit.argtypes = [cp, i32] + [vp] * 10
+        L.paep_cache_read_fourbit.restype = ctypes.c_int
+        L.paep_attend_fourbit_workspace_bytes.argtypes = [cp, ap]
+        L.paep_attend_fourbit_workspace_bytes.restype = sz
+        L.paep_attend_fourbit.argtypes = [cp, ap] + [vp] * 11 + [sz, vp]
+        L.paep_attend_fourbit.restype = ctypes.c_int
         L.paep_moe_workspace_bytes.argtypes = [mp]
         L.paep_moe_workspace_bytes.restype = sz
         L.paep_moe_layer.argtypes = [mp] + [vp] * 11 + [sz, vp]
@@ -849,6 +871,273 @@ def moe_experts(x: torch.Tensor, W13: torch.Tensor, W2: torch.Tensor, idx: torch
     if st != 0:
         raise PaepError(st, "paep_moe_experts")
     return y
+
+
+# ---- rotation of queries and keys, and a cache in 4 bits ----
+
+def _need_current(dev: int, stream) -> None:
+    """The library launches on the current device, and on a stream of it."""
+    if dev != torch.cuda.current_device() or (stream is not None and stream.device_index != dev):
+        raise ValueError("the tensors must be on the current device, and the stream one of its streams")
+
+
+def _need_plain(dev: int, dtype, name: str, t: torch.Tensor, shape) -> None:
+    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or t.shape != shape:
+        raise ValueError(f"{name} must be contiguous {dtype} {list(shape)}, on the device of the other tensors")
+
+
+def rotation_table(positions: int, rot: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
+    """The table [positions, rot] float32 for `rotate`: cosines and sines of position * base^(-2i / rot), i < rot / 2, from
+    angles in 64 bits.  (Any other table of that form will do.)"""
+    if positions < 1 or rot < 2 or rot % 2:
+        raise ValueError("positions must be at least 1, rot even and at least 2")
+    turn = float(base) ** (-torch.arange(0, rot, 2, dtype=torch.float64, device=device) / rot)
+    angle = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * turn
+    return torch.cat([angle.cos(), angle.sin()], dim=1).float()
+
+
+class Rotated(NamedTuple):
+    q: Optional[torch.Tensor]    # [n, Hq, D]
+    k: Optional[torch.Tensor]    # [n, Hk, D]
+
+
+def _rotate_bytes(q, k, positions, table, style, q_weight, k_weight, eps, q_out, k_out):
+    """Shape and type checks shared by rotate and rotate_append; the descriptor and the number of tokens."""
+    x = q if q is not None else k
+    if x is None:
+        raise ValueError("q or k must be given")
+    dev, dtype = x.get_device(), x.dtype
+    if dev < 0 or not x.is_cuda:
+        raise ValueError("every tensor must be a device tensor")
+    dt = _storage_dtype(x)
+    for name, t, out, weight in (("q", q, q_out, q_weight), ("k", k, k_out, k_weight)):
+        if t is None:
+            if weight is not None or out is not None:
+                raise ValueError(f"a weight or an output for {name}, but no {name}")
+            continue
+        if t.dim() != 3 or t.shape[0] != x.shape[0] or t.shape[2] != x.shape[2]:
+            raise ValueError("q and k must be [n, heads, D]")
+        _need_rows(dev, dtype, name, t)
+        if out is not None:
+            if out.shape != t.shape:
+                raise ValueError("out buffers have the wrong shape")
+            _need_rows(dev, dtype, "out." + name, out)
+        if weight is not None:
+            _need_plain(dev, dtype, name + "_weight", weight, (t.shape[2],))
+    n, _, D = x.shape
+    if table.dim() != 2:
+        raise ValueError("table must be [positions, rot]")
+    rows, rot = table.shape
+    _need_plain(dev, torch.float32, "table", table, (rows, rot))
+    _need_int32(dev, "positions", positions, (n,))
+    _need_32_bits("the number of tokens", n)
+    _need_32_bits("the number of the table's rows", rows)
+
+    def strides(t):
+        return (0, 0) if t is None else (_stride(t, 0), _stride(t, 1))
+    return _ROTATE_BYTES.pack(n, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], D, rot, rows, dt, ROTATE_STYLE[style],
+                              eps, 0, *strides(q), *strides(k), *strides(q_out), *strides(k_out)), dev
+
+
+def rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor, table: torch.Tensor, *, style: str = "halves",
+           q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+           out: Optional[Rotated] = None, stream=None) -> Rotated:
+    """Norm of each head and rotation by position, of queries q [n, Hq, D] and keys k [n, Hk, D] (any strides, the last
+    dimension contiguous; one of the two may be None) in one pass.
+
+    positions [n] int32 are rows of `table` [rows, rot] float32: cosines of the rot / 2 angles, then sines (`rotation_table`
+    makes one).  The first rot dimensions of a head are rotated: i with i + rot / 2 ("halves"), or 2i with 2i + 1 ("pairs").
+    With a weight [D] a head is x * weight / sqrt(mean(x^2) + eps) first.  Tokens at no row of the table are left out.
+    `out` may be Rotated(q, k) itself: in place."""
+    with _on(stream):
+        if out is None:
+            out = Rotated(*(None if t is None else t.new_empty(t.shape) for t in (q, k)))
+        elif (out.q is None) != (q is None) or (out.k is None) != (k is None):
+            raise ValueError("out buffers must be given for what is rotated")
+        desc, dev = _rotate_bytes(q, k, positions, table, style, q_weight, k_weight, eps, out.q, out.k)
+    _need_current(dev, stream)
+    st = lib().paep_rotate(desc, _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(positions), _ptr(table), _ptr(out.q),
+                           _ptr(out.k), _stream_ptr(stream))
+    if st != 0:
+        raise PaepError(st, "paep_rotate")
+    return out
+
+
+def rotate_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                  page_table: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, *, sequences: Optional[torch.Tensor] = None,
+                  angles: Optional[torch.Tensor] = None, style: str = "halves", q_weight: Optional[torch.Tensor] = None,
+                  k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, mass: Optional[torch.Tensor] = None,
+                  out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """`rotate` and `cache_append` in one pass: the keys go, rotated, to positions[i] of sequence sequences[i] (default: of
+    sequence i), the values v [n, Hk, Dv] with them; returns the rotated queries.  `angles` [n] int32: the rows of the table
+    where they are not the positions in the cache, as after an eviction.  `out`: the queries' buffer (q itself: in place)."""
+    c = _cache(k_pages, v_pages, page_table)
+    dev, n = c.dev, q.shape[0]
+    with _on(stream):
+        if out is None:
+            out = q.new_empty(q.shape)
+        desc, q_dev = _rotate_bytes(q, k, positions, table, style, q_weight, k_weight, eps, out, None)
+    if q_dev != dev or q.dtype is not k_pages.dtype:
+        raise ValueError("q, k and v must be of the cache's type and device")
+    if k.shape != (n, c.Hkv, c.Dk) or v.shape != (n, c.Hkv, c.Dv):
+        raise ValueError(f"k must be [n, {c.Hkv}, {c.Dk}] and v [n, {c.Hkv}, {c.Dv}]")
+    _need_rows(dev, k_pages.dtype, "v", v)
+    if sequences is not None:
+        _need_int32(dev, "sequences", sequences, (n,))
+    if angles is not None:
+        _need_int32(dev, "angles", angles, (n,))
+    if mass is not None:
+        _need_mass(dev, "mass", mass, c.B, c.Hkv, 0)
+    _need_current(dev, stream)
+    st = lib().paep_rotate_append(desc, c.desc, _ptr(q), _ptr(k), _ptr(v), _stride(v, 0), _stride(v, 1), _ptr(q_weight), _ptr(k_weight),
+                                  _ptr(table), _ptr(angles), _ptr(out), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(sequences),
+                                  _ptr(positions), _ptr(mass), 0 if mass is None else mass.shape[2], _stream_ptr(stream))
+    if st != 0:
+        raise PaepError(st, "paep_rotate_append")
+    return out
+
+
+def _fourbit_cache(k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor,
+                   page_table: torch.Tensor, dtype) -> _Cache:
+    """The cache in 4 bits: codes k_pages [n_pages, Hkv, page_size, Dk / 2], v_pages [n_pages, Hkv, page_size, Dv / 2] uint8 (any
+    strides, the last dimension contiguous), bytes k_scales [n_pages, Hkv, Dk / 32, page_size], v_scales likewise, page_table
+    [B, max_pages]; dtype: that of the tensors beside it."""
+    dev = k_pages.get_device()
+    if dev < 0 or not k_pages.is_cuda:
+        raise ValueError("every tensor must be a device tensor")
+    dt = BF16 if dtype is torch.bfloat16 else F32 if dtype is torch.float32 else None
+    if dt is None:
+        raise TypeError(f"unsupported storage dtype {dtype}; use float32 or bfloat16")
+    if k_pages.dim() != 4 or v_pages.dim() != 4 or k_pages.shape[:3] != v_pages.shape[:3] or page_table.dim() != 2:
+        raise ValueError(f"shape mismatch: k_pages{tuple(k_pages.shape)} v_pages{tuple(v_pages.shape)} page_table{tuple(page_table.shape)}")
+    n, H, ps, Dk = k_pages.shape
+    (kp, kh, ks, k1), (vp, vh, vs, v1) = k_pages.stride(), v_pages.stride()
+    if k1 != 1 or v1 != 1 or k_pages.dtype is not torch.uint8 or v_pages.dtype is not torch.uint8 or v_pages.get_device() != dev:
+        raise ValueError("k_pages and v_pages must be uint8 on one device, their last dimensions contiguous")
+    Dk, Dv = 2 * Dk, 2 * v_pages.shape[3]
+    _need_plain(dev, torch.uint8, "k_scales", k_scales, (n, H, Dk // 32, ps))
+    _need_plain(dev, torch.uint8, "v_scales", v_scales, (n, H, Dv // 32, ps))
+    _need_int32(dev, "page_table", page_table, None)
+    B, width = page_table.shape
+    if n < 2:                                                # (see _stride)
+        kp = vp = 0
+    if H < 2:
+        kh = vh = 0
+    if ps < 2:
+        ks = vs = 0
+    return _Cache(_CACHE_BYTES.pack(B, H, Dk, Dv, ps, n, width, dt, 2 * kp, 2 * kh, 2 * ks, 2 * vp, 2 * vh, 2 * vs), dev, B, H, Dk, Dv,
+                  min(width * ps, 0x7FFF0000))
+
+
+def cache_append_fourbit(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor,
+                         v_scales: torch.Tensor, page_table: torch.Tensor, positions: torch.Tensor, *,
+                         sequences: Optional[torch.Tensor] = None, stream=None) -> None:
+    """`cache_append` into a cache in 4 bits: k [n, Hkv, Dk] and v [n, Hkv, Dv], bf16 or float32 (any strides, the last dimension
+    contiguous; widths multiples of 32), are rounded, 32 neighbours sharing a power of two.
+
+    The codes are k_pages [n_pages, Hkv, page_size, Dk / 2], v_pages [n_pages, Hkv, page_size, Dv / 2] uint8, two to a byte, the
+    powers' exponents + 127 k_scales [n_pages, Hkv, Dk / 32, page_size], v_scales [n_pages, Hkv, Dv / 32, page_size] uint8."""
+    c = _fourbit_cache(k_pages, v_pages, k_scales, v_scales, page_table, k.dtype)
+    dev = c.dev
+    _need_rows(dev, k.dtype, "k", k)
+    _need_rows(dev, k.dtype, "v", v)
+    n = k.shape[0]
+    if k.shape != (n, c.Hkv, c.Dk) or v.shape != (n, c.Hkv, c.Dv):
+        raise ValueError(f"k must be [n, {c.Hkv}, {c.Dk}] and v [n, {c.Hkv}, {c.Dv}]")
+    _need_32_bits("the number of tokens", n)
+    _need_int32(dev, "positions", positions, (n,))
+    if sequences is not None:
+        _need_int32(dev, "sequences", sequences, (n,))
+    _need_current(dev, stream)
+    st = lib().paep_cache_append_fourbit(c.desc, n, _ptr(k), _stride(k, 0), _stride(k, 1), _ptr(v), _stride(v, 0), _stride(v, 1),
+                                         _ptr(k_pages), _ptr(v_pages), _ptr(k_scales), _ptr(v_scales), _ptr(page_table), _ptr(sequences),
+                                         _ptr(positions), _stream_ptr(stream))
+    if st != 0:
+        raise PaepError(st, "paep_cache_append_fourbit")
+
+
+class CacheRows(NamedTuple):
+    k: torch.Tensor           # [n, Hkv, Dk]
+    v: torch.Tensor           # [n, Hkv, Dv]
+
+
+def cache_read_fourbit(k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor,
+                       page_table: torch.Tensor, positions: torch.Tensor, *, sequences: Optional[torch.Tensor] = None,
+                       dtype: torch.dtype = torch.bfloat16, out: Optional[CacheRows] = None, stream=None) -> CacheRows:
+    """What stands in a cache in 4 bits (see `cache_append_fourbit`) at positions[i] of sequence sequences[i] (default: of
+    sequence i), exactly, in bf16 or float32; zeros where that names no place."""
+    if out is not None:
+        dtype = out.k.dtype
+    c = _fourbit_cache(k_pages, v_pages, k_scales, v_scales, page_table, dtype)
+    dev = c.dev
+    n = positions.numel()
+    _need_32_bits("the number of tokens", n)
+    _need_int32(dev, "positions", positions, (n,))
+    if sequences is not None:
+        _need_int32(dev, "sequences", sequences, (n,))
+    if out is None:
+        with _on(stream):
+            out = CacheRows(k_pages.new_empty((n, c.Hkv, c.Dk), dtype=dtype), k_pages.new_empty((n, c.Hkv, c.Dv), dtype=dtype))
+    else:
+        _need_plain(dev, dtype, "out.k", out.k, (n, c.Hkv, c.Dk))
+        _need_plain(dev, dtype, "out.v", out.v, (n, c.Hkv, c.Dv))
+    _need_current(dev, stream)
+    st = lib().paep_cache_read_fourbit(c.desc, n, _ptr(k_pages), _ptr(v_pages), _ptr(k_scales), _ptr(v_scales), _ptr(page_table),
+                                       _ptr(sequences), _ptr(positions), _ptr(out.k), _ptr(out.v), _stream_ptr(stream))
+    if st != 0:
+        raise PaepError(st, "paep_cache_read_fourbit")
+    return out
+
+
+def prepare_attend_fourbit(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor,
+                           page_table: torch.Tensor, lengths: torch.Tensor, *, scale: Optional[float] = None,
+                           starts: Optional[torch.Tensor] = None, max_len: Optional[int] = None, want_lse: bool = False,
+                           out: Optional[Attention] = None, workspace: Optional[torch.Tensor] = None) -> Prepared:
+    """Check and marshal one attend_fourbit call; the returned object runs it (see `attend_fourbit` for the arguments)."""
+    c = _fourbit_cache(k_pages, v_pages, k_scales, v_scales, page_table, q.dtype)
+    dev, B, dtype = c.dev, c.B, q.dtype
+    if q.dim() != 3 or q.shape[0] != B or q.shape[2] != c.Dk:
+        raise ValueError(f"q must be [{B}, heads, {c.Dk}]")
+    Hq = q.shape[1]
+    _need_rows(dev, dtype, "q", q)
+    _need_int32(dev, "lengths", lengths, (B,))
+    if starts is not None:
+        _need_int32(dev, "starts", starts, (B,))
+    if max_len is None:
+        max_len = c.capacity
+    else:
+        _need_32_bits("max_len", max_len)
+    if out is None:
+        out = Attention(q.new_empty((B, Hq, c.Dv)), q.new_empty((B, Hq), dtype=torch.float32) if want_lse else None)
+    else:
+        _need_plain(dev, dtype, "out.out", out.out, (B, Hq, c.Dv))
+        if out.lse is not None:
+            _need_plain(dev, torch.float32, "out.lse", out.lse, (B, Hq))
+    d = _ATTEND_BYTES.pack(Hq, max_len, c.Dk ** -0.5 if scale is None else scale, 0, _stride(q, 0), _stride(q, 1), 0)
+    L = lib()
+    need = L.paep_attend_fourbit_workspace_bytes(c.desc, d)
+    if workspace is None and need > 0:
+        workspace = q.new_empty(need, dtype=torch.uint8)
+    elif workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous tensor on the cache's device")
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    args = (c.desc, d, _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(k_scales), _ptr(v_scales), _ptr(page_table), _ptr(lengths),
+            _ptr(starts), _ptr(out.out), _ptr(out.lse), _ptr(workspace), ws_bytes)
+    return Prepared(L.paep_attend_fourbit, "paep_attend_fourbit", args,
+                    (q, k_pages, v_pages, k_scales, v_scales, page_table, lengths, starts, workspace), out)
+
+
+def attend_fourbit(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor,
+                   page_table: torch.Tensor, lengths: torch.Tensor, *, scale: Optional[float] = None,
+                   starts: Optional[torch.Tensor] = None, max_len: Optional[int] = None, want_lse: bool = False,
+                   out: Optional[Attention] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> Attention:
+    """`attend` over a cache in 4 bits (see `cache_append_fourbit` for its tensors), q and out in bf16 or float32; there is no
+    `mass`.  Nothing is rounded on the way from the cache to the sums."""
+    with _on(stream):
+        prep = prepare_attend_fourbit(q, k_pages, v_pages, k_scales, v_scales, page_table, lengths, scale=scale, starts=starts,
+                                      max_len=max_len, want_lse=want_lse, out=out, workspace=workspace)
+    _need_current(q.get_device(), stream)
+    return prep(stream)
 
 
 def probe_read(src: torch.Tensor, sink: torch.Tensor, stream=None) -> None:

@@ -1,5 +1,5 @@
-// C-ABI layer of a decode step's operators beside the predictor (attention over
-// a paged key-value cache, the cache's upkeep, the expert layer): argument
+// C-ABI layer of a decode step's operators beside the predictor (rotation,
+// attention over a paged key-value cache, the cache's upkeep, the expert layer): argument
 // validation on the host, before any HIP call, and dispatch.  See
 // include/paep.h for the contract of every entry point.
 #include "../../include/paep.h"
@@ -17,8 +17,8 @@ inline int element_bytes(int dtype) { return dtype == PAEP_F32 ? 4 : dtype == PA
 
 constexpr long long MAX_STRIDE = 1ll << 40;                  // elements: byte offsets of 2^31 pages stay below 2^63 with the checks below
 
-// strides of one pool: none overlaps the row it steps over, and the last page's offset fits in 62 bits
-paep_status check_strides(long long page, long long head, long long slot, int width, const paep_cache_desc* c)
+// strides of one pool: none overlaps the row it steps over, and the last page's offset fits in 62 bits; per16: elements in 16 bytes
+paep_status check_strides(long long page, long long head, long long slot, int width, const paep_cache_desc* c, int per16)
 {
     for (long long s : {page, head, slot})
         if (s < 0 || s > MAX_STRIDE) return PAEP_ERR_SHAPE;
@@ -26,20 +26,21 @@ paep_status check_strides(long long page, long long head, long long slot, int wi
         return PAEP_ERR_SHAPE;
     if (page > (1ll << 60) / c->n_pages || head > (1ll << 58) / c->Hkv || slot > (1ll << 58) / c->page_size)
         return PAEP_ERR_SHAPE;
-    const int per16 = 16 / element_bytes(c->dtype);
     return page % per16 || head % per16 || slot % per16 ? PAEP_ERR_ALIGN : PAEP_OK;
 }
 
-paep_status check_cache(const paep_cache_desc* c)
+// fourbit: the pools hold elements of 4 bits in groups of 32
+paep_status check_cache(const paep_cache_desc* c, bool fourbit = false)
 {
     if (!c) return PAEP_ERR_NULL;
     if (!element_bytes(c->dtype)) return PAEP_ERR_DTYPE;
     if (c->B < 0 || c->Hkv < 1 || c->Hkv > PAEP_MAX_HEADS || c->n_pages < 1 || c->max_pages < 1) return PAEP_ERR_SHAPE;
     for (int w : {c->Dk, c->Dv})
-        if (w < 8 || w > PAEP_MAX_HEAD_DIM || w % 8) return PAEP_ERR_SHAPE;
+        if (w < 8 || w > PAEP_MAX_HEAD_DIM || w % (fourbit ? 32 : 8)) return PAEP_ERR_SHAPE;
     if (c->page_size < 1 || c->page_size > 65536 || (c->page_size & (c->page_size - 1))) return PAEP_ERR_SHAPE;
-    const paep_status st = check_strides(c->k_page_stride, c->k_head_stride, c->k_slot_stride, c->Dk, c);
-    return st != PAEP_OK ? st : check_strides(c->v_page_stride, c->v_head_stride, c->v_slot_stride, c->Dv, c);
+    const int per16 = fourbit ? 32 : 16 / element_bytes(c->dtype);
+    const paep_status st = check_strides(c->k_page_stride, c->k_head_stride, c->k_slot_stride, c->Dk, c, per16);
+    return st != PAEP_OK ? st : check_strides(c->v_page_stride, c->v_head_stride, c->v_slot_stride, c->Dv, c, per16);
 }
 
 // positions are 32-bit in the kernels, with room for a tile past the last
@@ -63,9 +64,62 @@ paep::CacheView to_view(const paep_cache_desc* c, const void* k, const void* v, 
     return w;
 }
 
-paep_status check_attend(const paep_cache_desc* c, const paep_attend_desc* d, bool mass)
+// the same view with strides in bytes of codes
+paep::CacheView to_fourbit_view(const paep_cache_desc* c, const void* k, const void* v, const int32_t* table)
 {
-    const paep_status st = check_cache(c);
+    paep::CacheView w = to_view(c, k, v, table);
+    w.k_page = c->k_page_stride / 2; w.k_head = c->k_head_stride / 2; w.k_slot = c->k_slot_stride / 2;
+    w.v_page = c->v_page_stride / 2; w.v_head = c->v_head_stride / 2; w.v_slot = c->v_slot_stride / 2;
+    return w;
+}
+
+// strides between the rows of n tokens and between H heads of `width` in a tensor beside the cache; `out`: they may not overlap
+paep_status check_rows(long long row, long long head, int n, int H, int width, int dtype, bool out)
+{
+    for (long long s : {row, head})
+        if (s < 0 || s > MAX_STRIDE) return PAEP_ERR_SHAPE;
+    if (H > 1 && head < width) return PAEP_ERR_SHAPE;
+    if (n > 1 && out && row < width) return PAEP_ERR_SHAPE;
+    const int per16 = 16 / element_bytes(dtype);
+    return row % per16 || head % per16 ? PAEP_ERR_ALIGN : PAEP_OK;
+}
+
+paep_status check_rotate(const paep_rotate_desc* d, bool append)
+{
+    if (!d) return PAEP_ERR_NULL;
+    if (!element_bytes(d->dtype) || (d->style != PAEP_ROTATE_HALVES && d->style != PAEP_ROTATE_PAIRS)) return PAEP_ERR_DTYPE;
+    if (d->n < 0 || d->n > (1 << 24) || d->Hq < 0 || d->Hq > PAEP_MAX_HEADS || d->Hk < 0 || d->Hk > PAEP_MAX_HEADS || d->Hq + d->Hk < 1)
+        return PAEP_ERR_SHAPE;
+    if (d->D < 8 || d->D > PAEP_MAX_HEAD_DIM || d->D % 8 || d->rot < 2 || d->rot > d->D || d->rot % 2 || d->table_rows < 1 || d->reserved != 0)
+        return PAEP_ERR_SHAPE;
+    if (!isfinite(d->eps) || !(d->eps > 0.0f)) return PAEP_ERR_SHAPE;
+    paep_status st = PAEP_OK;
+    if (d->Hq > 0) {
+        st = check_rows(d->q_row_stride, d->q_head_stride, d->n, d->Hq, d->D, d->dtype, false);
+        if (st == PAEP_OK) st = check_rows(d->q_out_row_stride, d->q_out_head_stride, d->n, d->Hq, d->D, d->dtype, true);
+    }
+    if (d->Hk > 0) {
+        if (st == PAEP_OK) st = check_rows(d->k_row_stride, d->k_head_stride, d->n, d->Hk, d->D, d->dtype, false);
+        if (st == PAEP_OK && !append) st = check_rows(d->k_out_row_stride, d->k_out_head_stride, d->n, d->Hk, d->D, d->dtype, true);
+    }
+    return st;
+}
+
+paep::RotateArgs to_rotate(const paep_rotate_desc* d, bool append)
+{
+    const long long s = element_bytes(d->dtype);
+    paep::RotateArgs a{};
+    a.n = d->n; a.Hq = d->Hq; a.Hk = d->Hk; a.D = d->D; a.rot = d->rot; a.table_rows = d->table_rows; a.dtype = d->dtype; a.style = d->style;
+    a.eps = d->eps; a.append = append;
+    a.q_row = d->q_row_stride * s; a.q_head = d->q_head_stride * s; a.k_row = d->k_row_stride * s; a.k_head = d->k_head_stride * s;
+    a.q_out_row = d->q_out_row_stride * s; a.q_out_head = d->q_out_head_stride * s;
+    a.k_out_row = d->k_out_row_stride * s; a.k_out_head = d->k_out_head_stride * s;
+    return a;
+}
+
+paep_status check_attend(const paep_cache_desc* c, const paep_attend_desc* d, bool mass, bool fourbit = false)
+{
+    const paep_status st = check_cache(c, fourbit);
     if (st != PAEP_OK) return st;
     if (!d) return PAEP_ERR_NULL;
     if (d->Hq < 1 || d->Hq > PAEP_MAX_HEADS || d->Hq % c->Hkv || d->reserved != 0) return PAEP_ERR_SHAPE;
@@ -212,6 +266,133 @@ paep_status paep_cache_evict(const paep_cache_desc* cache, int32_t max_len, int3
                                                     kept_dev, mass_out_dev, mass_out_stride, lengths_out_dev,
                                                     static_cast<hipStream_t>(stream));
     return err == hipSuccess ? PAEP_OK : PAEP_ERR_HIP;
+}
+
+size_t paep_attend_fourbit_workspace_bytes(const paep_cache_desc* cache, const paep_attend_desc* desc)
+{
+    if (check_attend(cache, desc, false, true) != PAEP_OK) return 0;
+    const paep::AttendFourbitArgs a{to_attend(cache, desc, nullptr, nullptr, nullptr), nullptr, nullptr};
+    return paep::attend_fourbit_fits(a) ? paep::attend_fourbit_workspace_bytes(a) : 0;
+}
+
+paep_status paep_attend_fourbit(const paep_cache_desc* cache, const paep_attend_desc* desc, const void* q_dev,
+                            const void* k_pages_dev, const void* v_pages_dev, const uint8_t* k_scales_dev,
+                            const uint8_t* v_scales_dev, const int32_t* page_table_dev, const int32_t* lengths_dev,
+                            const int32_t* starts_dev, void* out_dev, float* lse_dev,
+                            void* workspace_dev, size_t workspace_bytes, void* stream)
+{
+    const paep_status st = check_attend(cache, desc, false, true);
+    if (st != PAEP_OK) return st;
+    if (!k_pages_dev || !v_pages_dev || !k_scales_dev || !v_scales_dev) return PAEP_ERR_NULL;
+    if (cache->B > 0 && (!q_dev || !page_table_dev || !lengths_dev || !out_dev)) return PAEP_ERR_NULL;
+    for (const void* p : {q_dev, k_pages_dev, v_pages_dev, (const void*)k_scales_dev, (const void*)v_scales_dev, (const void*)out_dev})
+        if (!aligned16(p)) return PAEP_ERR_ALIGN;
+    paep::AttendFourbitArgs f{to_attend(cache, desc, k_pages_dev, v_pages_dev, page_table_dev), k_scales_dev, v_scales_dev};
+    f.a.c = to_fourbit_view(cache, k_pages_dev, v_pages_dev, page_table_dev);
+    if (!paep::attend_fourbit_fits(f)) return PAEP_ERR_SHAPE;
+    const size_t need = paep::attend_fourbit_workspace_bytes(f);
+    if (need > 0 && (!workspace_dev || !aligned16(workspace_dev) || workspace_bytes < need)) return PAEP_ERR_WORKSPACE;
+    if (cache->B == 0) return PAEP_OK;
+    f.a.q = q_dev; f.a.lengths = lengths_dev; f.a.starts = starts_dev; f.a.out = out_dev; f.a.lse = lse_dev;
+    f.a.workspace = workspace_dev;
+    f.a.stream = static_cast<hipStream_t>(stream);
+    return paep::launch_attend_fourbit(f) == hipSuccess ? PAEP_OK : PAEP_ERR_HIP;
+}
+
+paep_status paep_cache_append_fourbit(const paep_cache_desc* cache, int32_t n, const void* k_dev, int64_t k_row_stride,
+                                  int64_t k_head_stride, const void* v_dev, int64_t v_row_stride, int64_t v_head_stride,
+                                  void* k_pages_dev, void* v_pages_dev, uint8_t* k_scales_dev, uint8_t* v_scales_dev,
+                                  const int32_t* page_table_dev, const int32_t* sequences_dev, const int32_t* positions_dev,
+                                  void* stream)
+{
+    paep_status st = check_cache(cache, true);
+    if (st != PAEP_OK) return st;
+    if (n < 0 || n > (1 << 24) || (!sequences_dev && n > cache->B)) return PAEP_ERR_SHAPE;
+    st = check_rows(k_row_stride, k_head_stride, n, cache->Hkv, cache->Dk, cache->dtype, false);
+    if (st == PAEP_OK) st = check_rows(v_row_stride, v_head_stride, n, cache->Hkv, cache->Dv, cache->dtype, false);
+    if (st != PAEP_OK) return st;
+    if (!k_pages_dev || !v_pages_dev || !k_scales_dev || !v_scales_dev) return PAEP_ERR_NULL;
+    if (n > 0 && (!k_dev || !v_dev || !positions_dev || (cache->B > 0 && !page_table_dev))) return PAEP_ERR_NULL;
+    for (const void* p : {k_dev, v_dev, (const void*)k_pages_dev, (const void*)v_pages_dev, (const void*)k_scales_dev, (const void*)v_scales_dev})
+        if (!aligned16(p)) return PAEP_ERR_ALIGN;
+    if (n == 0 || cache->B == 0) return PAEP_OK;
+    const long long s = element_bytes(cache->dtype);
+    const hipError_t err = paep::launch_cache_append_fourbit(to_fourbit_view(cache, k_pages_dev, v_pages_dev, page_table_dev), k_scales_dev,
+                                                         v_scales_dev, n, k_dev, k_row_stride * s, k_head_stride * s, v_dev,
+                                                         v_row_stride * s, v_head_stride * s, sequences_dev, positions_dev,
+                                                         static_cast<hipStream_t>(stream));
+    return err == hipSuccess ? PAEP_OK : PAEP_ERR_HIP;
+}
+
+paep_status paep_cache_read_fourbit(const paep_cache_desc* cache, int32_t n, const void* k_pages_dev, const void* v_pages_dev,
+                                const uint8_t* k_scales_dev, const uint8_t* v_scales_dev, const int32_t* page_table_dev,
+                                const int32_t* sequences_dev, const int32_t* positions_dev, void* k_out_dev, void* v_out_dev,
+                                void* stream)
+{
+    const paep_status st = check_cache(cache, true);
+    if (st != PAEP_OK) return st;
+    if (n < 0 || n > (1 << 24) || (!sequences_dev && n > cache->B)) return PAEP_ERR_SHAPE;
+    if (!k_pages_dev || !v_pages_dev || !k_scales_dev || !v_scales_dev) return PAEP_ERR_NULL;
+    if (n > 0 && (!positions_dev || !k_out_dev || !v_out_dev || (cache->B > 0 && !page_table_dev))) return PAEP_ERR_NULL;
+    for (const void* p : {k_pages_dev, v_pages_dev, (const void*)k_scales_dev, (const void*)v_scales_dev, (const void*)k_out_dev, (const void*)v_out_dev})
+        if (!aligned16(p)) return PAEP_ERR_ALIGN;
+    if (n == 0) return PAEP_OK;
+    const hipError_t err = paep::launch_cache_read_fourbit(to_fourbit_view(cache, k_pages_dev, v_pages_dev, page_table_dev), k_scales_dev,
+                                                       v_scales_dev, n, sequences_dev, positions_dev, k_out_dev, v_out_dev,
+                                                       static_cast<hipStream_t>(stream));
+    return err == hipSuccess ? PAEP_OK : PAEP_ERR_HIP;
+}
+
+paep_status paep_rotate(const paep_rotate_desc* desc, const void* q_dev, const void* k_dev,
+                        const void* q_weight_dev, const void* k_weight_dev, const int32_t* positions_dev,
+                        const float* table_dev, void* q_out_dev, void* k_out_dev, void* stream)
+{
+    const paep_status st = check_rotate(desc, false);
+    if (st != PAEP_OK) return st;
+    if (!table_dev) return PAEP_ERR_NULL;
+    if (desc->n > 0 && (!positions_dev || (desc->Hq > 0 && (!q_dev || !q_out_dev)) || (desc->Hk > 0 && (!k_dev || !k_out_dev)))) return PAEP_ERR_NULL;
+    for (const void* p : {q_dev, k_dev, q_weight_dev, k_weight_dev, (const void*)table_dev, (const void*)q_out_dev, (const void*)k_out_dev})
+        if (!aligned16(p)) return PAEP_ERR_ALIGN;
+    if (desc->n == 0) return PAEP_OK;
+    paep::RotateArgs a = to_rotate(desc, false);
+    a.q = q_dev; a.k = k_dev; a.q_out = q_out_dev; a.k_out = k_out_dev; a.q_weight = q_weight_dev; a.k_weight = k_weight_dev;
+    a.angles = positions_dev; a.table = table_dev;
+    a.stream = static_cast<hipStream_t>(stream);
+    return paep::launch_rotate(a) == hipSuccess ? PAEP_OK : PAEP_ERR_HIP;
+}
+
+paep_status paep_rotate_append(const paep_rotate_desc* desc, const paep_cache_desc* cache, const void* q_dev,
+                               const void* k_dev, const void* v_dev, int64_t v_row_stride, int64_t v_head_stride,
+                               const void* q_weight_dev, const void* k_weight_dev, const float* table_dev,
+                               const int32_t* angles_dev, void* q_out_dev, void* k_pages_dev, void* v_pages_dev,
+                               const int32_t* page_table_dev, const int32_t* sequences_dev, const int32_t* positions_dev,
+                               float* mass_dev, int64_t mass_stride, void* stream)
+{
+    paep_status st = check_rotate(desc, true);
+    if (st == PAEP_OK) st = check_cache(cache);
+    if (st != PAEP_OK) return st;
+    if (cache->Hkv != desc->Hk || cache->Dk != desc->D) return PAEP_ERR_SHAPE;
+    if (cache->dtype != desc->dtype) return PAEP_ERR_DTYPE;
+    if (!sequences_dev && desc->n > cache->B) return PAEP_ERR_SHAPE;
+    st = check_rows(v_row_stride, v_head_stride, desc->n, cache->Hkv, cache->Dv, cache->dtype, false);
+    if (st != PAEP_OK) return st;
+    if (mass_dev && (mass_stride < 0 || mass_stride > MAX_STRIDE)) return PAEP_ERR_SHAPE;
+    if (!table_dev || !k_pages_dev || !v_pages_dev) return PAEP_ERR_NULL;
+    if (desc->n > 0 && (!k_dev || !v_dev || !positions_dev || (desc->Hq > 0 && (!q_dev || !q_out_dev)) || (cache->B > 0 && !page_table_dev)))
+        return PAEP_ERR_NULL;
+    for (const void* p : {q_dev, k_dev, v_dev, q_weight_dev, k_weight_dev, (const void*)table_dev, (const void*)q_out_dev,
+                          (const void*)k_pages_dev, (const void*)v_pages_dev})
+        if (!aligned16(p)) return PAEP_ERR_ALIGN;
+    if (desc->n == 0) return PAEP_OK;
+    paep::RotateArgs a = to_rotate(desc, true);
+    a.c = to_view(cache, k_pages_dev, v_pages_dev, page_table_dev);
+    a.q = q_dev; a.k = k_dev; a.v = v_dev; a.q_out = q_out_dev; a.q_weight = q_weight_dev; a.k_weight = k_weight_dev;
+    const long long s = element_bytes(desc->dtype);
+    a.v_row = v_row_stride * s; a.v_head = v_head_stride * s;
+    a.angles = angles_dev ? angles_dev : positions_dev; a.table = table_dev;
+    a.sequences = sequences_dev; a.positions = positions_dev; a.mass = mass_dev; a.mass_stride = mass_stride;
+    a.stream = static_cast<hipStream_t>(stream);
+    return paep::launch_rotate(a) == hipSuccess ? PAEP_OK : PAEP_ERR_HIP;
 }
 
 size_t paep_moe_workspace_bytes(const paep_moe_desc* desc)

@@ -133,6 +133,16 @@ bool attend_fits(const AttendArgs& a);                       // the grid holds t
 size_t attend_workspace_bytes(const AttendArgs& a);          // (a.mass: whether there is one)
 hipError_t launch_attend(const AttendArgs& a);
 
+// over a cache in 4 bits: strides of the view count bytes of codes; its dtype is that of q and out
+struct AttendFourbitArgs {
+    AttendArgs a;
+    const uint8_t* k_scales;       // [n_pages][Hkv][Dk / 32][page size]
+    const uint8_t* v_scales;
+};
+bool attend_fourbit_fits(const AttendFourbitArgs& a);
+size_t attend_fourbit_workspace_bytes(const AttendFourbitArgs& a);
+hipError_t launch_attend_fourbit(const AttendFourbitArgs& a);
+
 hipError_t launch_cache_append(const CacheView& c, int n, const void* k, long long k_row, const void* v, long long v_row,
                                const int32_t* sequences, const int32_t* positions, float* mass, long long mass_stride,
                                hipStream_t stream);
@@ -140,6 +150,39 @@ hipError_t launch_cache_evict(const CacheView& c, int max_len, int budget, int r
                               const float* mass, long long mass_stride, const int32_t* out_table, int out_max_pages,
                               int32_t* kept, float* mass_out, long long mass_out_stride, int32_t* lengths_out,
                               hipStream_t stream);
+
+// the same for a cache in 4 bits (scales as in AttendFourbitArgs; strides of k and v in bytes)
+hipError_t launch_cache_append_fourbit(const CacheView& c, uint8_t* k_scales, uint8_t* v_scales, int n, const void* k, long long k_row,
+                                   long long k_head, const void* v, long long v_row, long long v_head, const int32_t* sequences,
+                                   const int32_t* positions, hipStream_t stream);
+hipError_t launch_cache_read_fourbit(const CacheView& c, const uint8_t* k_scales, const uint8_t* v_scales, int n, const int32_t* sequences,
+                                 const int32_t* positions, void* k, void* v, hipStream_t stream);
+
+// norms and rotation of queries and keys; append: the keys, and the values, go into the cache
+struct RotateArgs {
+    int n, Hq, Hk, D, rot, table_rows, dtype, style;
+    float eps;
+    bool append;
+    const void* q;
+    const void* k;
+    void* q_out;
+    void* k_out;                   // (without append)
+    long long q_row, q_head, k_row, k_head, q_out_row, q_out_head, k_out_row, k_out_head;      // bytes
+    const void* q_weight;          // nullable: no norm
+    const void* k_weight;
+    const int32_t* angles;         // rows of the table
+    const float* table;            // [table_rows][rot]
+    // with append
+    CacheView c;
+    const void* v;
+    long long v_row, v_head;       // bytes
+    const int32_t* sequences;      // nullable
+    const int32_t* positions;
+    float* mass;                   // nullable
+    long long mass_stride;
+    hipStream_t stream;
+};
+hipError_t launch_rotate(const RotateArgs& a);
 
 struct MoeArgs {
     int T, d, f, E, k, dtype, act, prob_mode;
