@@ -875,10 +875,15 @@ def moe_experts(x: torch.Tensor, W13: torch.Tensor, W2: torch.Tensor, idx: torch
 
 # ---- rotation of queries and keys, and a cache in 4 bits ----
 
-def _need_current(dev: int, stream) -> None:
-    """The library launches on the current device, and on a stream of it."""
-    if dev != torch.cuda.current_device() or (stream is not None and stream.device_index != dev):
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _launch_stream(dev: int, stream) -> int:
+    """The stream for a launch on the tensors' device, which has to be the current one."""
+    if dev != _get_device() or (stream is not None and stream.device_index != dev):
         raise ValueError("the tensors must be on the current device, and the stream one of its streams")
+    return stream.cuda_stream if stream is not None else _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
 
 
 def _need_plain(dev: int, dtype, name: str, t: torch.Tensor, shape) -> None:
@@ -901,42 +906,55 @@ class Rotated(NamedTuple):
     k: Optional[torch.Tensor]    # [n, Hk, D]
 
 
+def _need_heads(dev: int, dtype, name: str, t: torch.Tensor, n: int, D: int, out, weight) -> None:
+    """Heads [n, any, D] of one type and device, their outputs and the weight of their norm."""
+    if t.dim() != 3 or t.shape[0] != n or t.shape[2] != D:
+        raise ValueError("q and k must be [n, heads, D]")
+    _need_rows(dev, dtype, name, t)
+    if out is not None:
+        if out.shape != t.shape:
+            raise ValueError("out buffers have the wrong shape")
+        _need_rows(dev, dtype, "out." + name, out)
+    if weight is not None:
+        _need_plain(dev, dtype, name + "_weight", weight, (D,))
+
+
 def _rotate_bytes(q, k, positions, table, style, q_weight, k_weight, eps, q_out, k_out):
-    """Shape and type checks shared by rotate and rotate_append; the descriptor and the number of tokens."""
+    """Shape and type checks shared by rotate and rotate_append; the descriptor and the device."""
     x = q if q is not None else k
     if x is None:
         raise ValueError("q or k must be given")
     dev, dtype = x.get_device(), x.dtype
     if dev < 0 or not x.is_cuda:
         raise ValueError("every tensor must be a device tensor")
-    dt = _storage_dtype(x)
-    for name, t, out, weight in (("q", q, q_out, q_weight), ("k", k, k_out, k_weight)):
-        if t is None:
-            if weight is not None or out is not None:
-                raise ValueError(f"a weight or an output for {name}, but no {name}")
-            continue
-        if t.dim() != 3 or t.shape[0] != x.shape[0] or t.shape[2] != x.shape[2]:
-            raise ValueError("q and k must be [n, heads, D]")
-        _need_rows(dev, dtype, name, t)
-        if out is not None:
-            if out.shape != t.shape:
-                raise ValueError("out buffers have the wrong shape")
-            _need_rows(dev, dtype, "out." + name, out)
-        if weight is not None:
-            _need_plain(dev, dtype, name + "_weight", weight, (t.shape[2],))
-    n, _, D = x.shape
-    if table.dim() != 2:
-        raise ValueError("table must be [positions, rot]")
-    rows, rot = table.shape
-    _need_plain(dev, torch.float32, "table", table, (rows, rot))
+    if x.dim() != 3 or table.dim() != 2:
+        raise ValueError("q and k must be [n, heads, D], table [positions, rot]")
+    (n, _, D), (rows, rot) = x.shape, table.shape
+    Hq = Hk = qr = qh = kr = kh = qor = qoh = kor = koh = 0
+    if q is not None:
+        _need_heads(dev, dtype, "q", q, n, D, q_out, q_weight)
+        Hq, (qr, qh, _), (qor, qoh, _) = q.shape[1], q.stride(), q_out.stride()
+    elif q_weight is not None or q_out is not None:
+        raise ValueError("a weight or an output for q, but no q")
+    if k is not None:
+        _need_heads(dev, dtype, "k", k, n, D, k_out, k_weight)
+        Hk, (kr, kh, _) = k.shape[1], k.stride()
+        if k_out is not None:
+            kor, koh, _ = k_out.stride()
+    elif k_weight is not None or k_out is not None:
+        raise ValueError("a weight or an output for k, but no k")
+    if n < 2:                                                # (see _stride)
+        qr = kr = qor = kor = 0
+    if Hq < 2:
+        qh = qoh = 0
+    if Hk < 2:
+        kh = koh = 0
+    if table.dtype is not torch.float32 or table.get_device() != dev or not table.is_contiguous():
+        raise ValueError("table must be contiguous float32, on the device of the other tensors")
     _need_int32(dev, "positions", positions, (n,))
-    _need_32_bits("the number of tokens", n)
-    _need_32_bits("the number of the table's rows", rows)
-
-    def strides(t):
-        return (0, 0) if t is None else (_stride(t, 0), _stride(t, 1))
-    return _ROTATE_BYTES.pack(n, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], D, rot, rows, dt, ROTATE_STYLE[style],
-                              eps, 0, *strides(q), *strides(k), *strides(q_out), *strides(k_out)), dev
+    if n >= 1 << 31 or rows >= 1 << 31:
+        raise ValueError("the number of tokens and of the table's rows must fit in 32 bits")
+    return _ROTATE_BYTES.pack(n, Hq, Hk, D, rot, rows, _storage_dtype(x), ROTATE_STYLE[style], eps, 0, qr, qh, kr, kh, qor, qoh, kor, koh), dev
 
 
 def rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor, table: torch.Tensor, *, style: str = "halves",
@@ -949,15 +967,15 @@ def rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torc
     makes one).  The first rot dimensions of a head are rotated: i with i + rot / 2 ("halves"), or 2i with 2i + 1 ("pairs").
     With a weight [D] a head is x * weight / sqrt(mean(x^2) + eps) first.  Tokens at no row of the table are left out.
     `out` may be Rotated(q, k) itself: in place."""
-    with _on(stream):
-        if out is None:
-            out = Rotated(*(None if t is None else t.new_empty(t.shape) for t in (q, k)))
-        elif (out.q is None) != (q is None) or (out.k is None) != (k is None):
-            raise ValueError("out buffers must be given for what is rotated")
-        desc, dev = _rotate_bytes(q, k, positions, table, style, q_weight, k_weight, eps, out.q, out.k)
-    _need_current(dev, stream)
-    st = lib().paep_rotate(desc, _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(positions), _ptr(table), _ptr(out.q),
-                           _ptr(out.k), _stream_ptr(stream))
+    if out is None:
+        with _on(stream):
+            out = Rotated(None if q is None else q.new_empty(q.shape), None if k is None else k.new_empty(k.shape))
+    elif (out.q is None) != (q is None) or (out.k is None) != (k is None):
+        raise ValueError("out buffers must be given for what is rotated")
+    desc, dev = _rotate_bytes(q, k, positions, table, style, q_weight, k_weight, eps, out.q, out.k)
+    raw = _launch_stream(dev, stream)
+    st = lib().paep_rotate(desc, _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), positions.data_ptr(), table.data_ptr(), _ptr(out.q),
+                           _ptr(out.k), raw)
     if st != 0:
         raise PaepError(st, "paep_rotate")
     return out
@@ -973,10 +991,10 @@ def rotate_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_pages: to
     where they are not the positions in the cache, as after an eviction.  `out`: the queries' buffer (q itself: in place)."""
     c = _cache(k_pages, v_pages, page_table)
     dev, n = c.dev, q.shape[0]
-    with _on(stream):
-        if out is None:
+    if out is None:
+        with _on(stream):
             out = q.new_empty(q.shape)
-        desc, q_dev = _rotate_bytes(q, k, positions, table, style, q_weight, k_weight, eps, out, None)
+    desc, q_dev = _rotate_bytes(q, k, positions, table, style, q_weight, k_weight, eps, out, None)
     if q_dev != dev or q.dtype is not k_pages.dtype:
         raise ValueError("q, k and v must be of the cache's type and device")
     if k.shape != (n, c.Hkv, c.Dk) or v.shape != (n, c.Hkv, c.Dv):
@@ -988,10 +1006,11 @@ def rotate_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_pages: to
         _need_int32(dev, "angles", angles, (n,))
     if mass is not None:
         _need_mass(dev, "mass", mass, c.B, c.Hkv, 0)
-    _need_current(dev, stream)
-    st = lib().paep_rotate_append(desc, c.desc, _ptr(q), _ptr(k), _ptr(v), _stride(v, 0), _stride(v, 1), _ptr(q_weight), _ptr(k_weight),
-                                  _ptr(table), _ptr(angles), _ptr(out), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(sequences),
-                                  _ptr(positions), _ptr(mass), 0 if mass is None else mass.shape[2], _stream_ptr(stream))
+    raw = _launch_stream(dev, stream)
+    st = lib().paep_rotate_append(desc, c.desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), _stride(v, 0), _stride(v, 1), _ptr(q_weight),
+                                  _ptr(k_weight), table.data_ptr(), _ptr(angles), out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+                                  page_table.data_ptr(), _ptr(sequences), positions.data_ptr(), _ptr(mass),
+                                  0 if mass is None else mass.shape[2], raw)
     if st != 0:
         raise PaepError(st, "paep_rotate_append")
     return out
@@ -1015,8 +1034,9 @@ def _fourbit_cache(k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch
     if k1 != 1 or v1 != 1 or k_pages.dtype is not torch.uint8 or v_pages.dtype is not torch.uint8 or v_pages.get_device() != dev:
         raise ValueError("k_pages and v_pages must be uint8 on one device, their last dimensions contiguous")
     Dk, Dv = 2 * Dk, 2 * v_pages.shape[3]
-    _need_plain(dev, torch.uint8, "k_scales", k_scales, (n, H, Dk // 32, ps))
-    _need_plain(dev, torch.uint8, "v_scales", v_scales, (n, H, Dv // 32, ps))
+    for t, D in ((k_scales, Dk), (v_scales, Dv)):
+        if t.dtype is not torch.uint8 or t.get_device() != dev or not t.is_contiguous() or t.shape != (n, H, D // 32, ps):
+            raise ValueError("k_scales must be contiguous uint8 [n_pages, Hkv, Dk / 32, page_size] on the cache's device, v_scales likewise")
     _need_int32(dev, "page_table", page_table, None)
     B, width = page_table.shape
     if n < 2:                                                # (see _stride)
@@ -1048,10 +1068,10 @@ def cache_append_fourbit(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor
     _need_int32(dev, "positions", positions, (n,))
     if sequences is not None:
         _need_int32(dev, "sequences", sequences, (n,))
-    _need_current(dev, stream)
-    st = lib().paep_cache_append_fourbit(c.desc, n, _ptr(k), _stride(k, 0), _stride(k, 1), _ptr(v), _stride(v, 0), _stride(v, 1),
-                                         _ptr(k_pages), _ptr(v_pages), _ptr(k_scales), _ptr(v_scales), _ptr(page_table), _ptr(sequences),
-                                         _ptr(positions), _stream_ptr(stream))
+    raw = _launch_stream(dev, stream)
+    st = lib().paep_cache_append_fourbit(c.desc, n, k.data_ptr(), _stride(k, 0), _stride(k, 1), v.data_ptr(), _stride(v, 0), _stride(v, 1),
+                                         k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(),
+                                         page_table.data_ptr(), _ptr(sequences), positions.data_ptr(), raw)
     if st != 0:
         raise PaepError(st, "paep_cache_append_fourbit")
 
@@ -1071,19 +1091,19 @@ def cache_read_fourbit(k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: t
     c = _fourbit_cache(k_pages, v_pages, k_scales, v_scales, page_table, dtype)
     dev = c.dev
     n = positions.numel()
-    _need_32_bits("the number of tokens", n)
     _need_int32(dev, "positions", positions, (n,))
     if sequences is not None:
         _need_int32(dev, "sequences", sequences, (n,))
+    _need_32_bits("the number of tokens", n)
     if out is None:
         with _on(stream):
             out = CacheRows(k_pages.new_empty((n, c.Hkv, c.Dk), dtype=dtype), k_pages.new_empty((n, c.Hkv, c.Dv), dtype=dtype))
     else:
         _need_plain(dev, dtype, "out.k", out.k, (n, c.Hkv, c.Dk))
         _need_plain(dev, dtype, "out.v", out.v, (n, c.Hkv, c.Dv))
-    _need_current(dev, stream)
-    st = lib().paep_cache_read_fourbit(c.desc, n, _ptr(k_pages), _ptr(v_pages), _ptr(k_scales), _ptr(v_scales), _ptr(page_table),
-                                       _ptr(sequences), _ptr(positions), _ptr(out.k), _ptr(out.v), _stream_ptr(stream))
+    raw = _launch_stream(dev, stream)
+    st = lib().paep_cache_read_fourbit(c.desc, n, k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(),
+                                       page_table.data_ptr(), _ptr(sequences), positions.data_ptr(), out.k.data_ptr(), out.v.data_ptr(), raw)
     if st != 0:
         raise PaepError(st, "paep_cache_read_fourbit")
     return out
@@ -1136,7 +1156,7 @@ def attend_fourbit(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor
     with _on(stream):
         prep = prepare_attend_fourbit(q, k_pages, v_pages, k_scales, v_scales, page_table, lengths, scale=scale, starts=starts,
                                       max_len=max_len, want_lse=want_lse, out=out, workspace=workspace)
-    _need_current(q.get_device(), stream)
+    _launch_stream(q.get_device(), stream)
     return prep(stream)
 
 
