@@ -295,3 +295,20 @@ def test_python_calls_refuse():
     assert not bool(B.cache_read_fourbit(kp, kp, ks, ks, none, pos, sequences=pos).k.any())
     B.cache_append_fourbit(x, x, kp, kp, ks, ks, none, pos, sequences=pos)
     assert not bool(kp.any())
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [4095, 8198])
+def test_many_tokens_at_once(kind, n):
+    """Threads that work on several tokens each: as one token after the other, the last ones and skipped ones among them."""
+    g = torch.Generator(device="cuda").manual_seed(n)
+    c = Cache(g, 3, 8, 128, 160, 16, 200, "slots")
+    k, v = (torch.randn((n, 8, D), generator=g, device="cuda").to(TYPES[kind]) for D in (128, 160))
+    seq, pos = (torch.arange(n, device="cuda") % 3).to(torch.int32), (torch.arange(n, device="cuda") // 3).to(torch.int32)
+    pos[5::7] = -1
+    B.cache_append_fourbit(k, v, *c.tensors, pos, sequences=seq)
+    got = B.cache_read_fourbit(*c.tensors, pos, sequences=seq, dtype=TYPES[kind])
+    here = (pos >= 0).cpu().numpy()
+    for x, y in ((k, got.k), (v, got.v)):
+        want, _ = R.to_fourbit(x.float().cpu().numpy()[here])
+        assert np.array_equal(_np(y)[here], want) and not _np(y)[~here].any()
