@@ -191,6 +191,28 @@ def test_many_tokens_and_positions_far_out():
         _check(y, want, tol, "rows")
 
 
+@pytest.mark.parametrize("kind,n", [("bf16", 8200), ("f32", 4111)])
+def test_results_written_past_the_caches_are_the_same(kind, n):
+    """Calls large enough for that, in place too, and their rows in a smaller call."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    q, k = _rows(g, n, 32, 128, TYPES[kind]), _rows(g, n, 2, 128, TYPES[kind])
+    w, turns = torch.randn(128, generator=g, device="cuda").to(TYPES[kind]), B.rotation_table(n, 128)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    pos[7] = -1
+    out = B.Rotated(torch.zeros_like(q), torch.zeros_like(k))
+    B.rotate(q, k, pos, turns, q_weight=w, k_weight=w, out=out)
+    part = slice(n - 600, n)
+    few = B.rotate(q[part], k[part], pos[part].contiguous(), turns, q_weight=w, k_weight=w)
+    assert torch.equal(out.q[part], few.q) and torch.equal(out.k[part], few.k) and not bool(out.q[7].any())
+    want, tol = R.rotate(_np(q[:300]), _np(w), turns[pos[:300].clamp(min=0).long()].cpu().numpy(), "halves", float(np.float32(1e-6)), kind)
+    want[7] = 0
+    _check(out.q[:300], want, tol, "rows")
+    seventh = q[7].clone()
+    B.rotate(q, k, pos, turns, q_weight=w, k_weight=w, out=B.Rotated(q, k))
+    out.q[7] = seventh
+    assert torch.equal(q, out.q)
+
+
 def test_python_calls_refuse():
     q, k, turns = torch.zeros((3, 4, 32), device="cuda"), torch.zeros((3, 2, 32), device="cuda"), B.rotation_table(8, 32)
     pos, w = _i32(0, 1, 2), torch.ones(32, device="cuda")
