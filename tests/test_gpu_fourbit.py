@@ -312,3 +312,31 @@ def test_many_tokens_at_once(kind, n):
     for x, y in ((k, got.k), (v, got.v)):
         want, _ = R.to_fourbit(x.float().cpu().numpy()[here])
         assert np.array_equal(_np(y)[here], want) and not _np(y)[~here].any()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_attend_more_sequences_than_one_launch_takes(kind):
+    g = torch.Generator(device="cuda").manual_seed(21)
+    n, ps = 1500, 16
+    c = Cache(g, n, 1, 32, 32, ps, 20, spare=0)
+    lengths = torch.randint(0, 320, (n,), generator=g, device="cuda").to(torch.int32)
+    lengths[1023:1026], lengths[0], lengths[-1] = 320, 0, 0
+    starts = torch.where(torch.arange(n, device="cuda") % 3 == 0, lengths // 2, 0).to(torch.int32)
+    q = torch.randn((n, 2, 32), generator=g, device="cuda").to(TYPES[kind])
+    got = B.attend_fourbit(q, *c.tensors, lengths, starts=starts, want_lse=True)
+    want, tol = R.attend(_np(q), *c.values(), c.table.cpu().numpy(), lengths.tolist(), starts.tolist(), float(np.float32(32 ** -0.5)), 320, kind)
+    none = ~np.isfinite(want[1])
+    lse = _np(got.lse)
+    assert np.all(np.abs(_np(got.out) - want[0]) <= tol[0]) and np.array_equal(none, lse == -np.inf)
+    assert np.all(np.abs(lse[~none] - want[1][~none]) <= tol[1][~none])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_attend_joins_more_pieces_than_fit_at_once(kind):
+    g = torch.Generator(device="cuda").manual_seed(22)
+    c = Cache(g, 2, 1, 64, 96, 64, 2200, spare=0)
+    q = torch.randn((2, 3, 64), generator=g, device="cuda").to(TYPES[kind])
+    lengths, k_v = [140001, 700], c.values()
+    got = B.attend_fourbit(q, *c.tensors, _i32(*lengths), want_lse=True)
+    want, tol = R.attend(_np(q), *k_v, c.table.cpu().numpy(), lengths, None, 0.125, 140800, kind)
+    assert np.all(np.abs(_np(got.out) - want[0]) <= tol[0]) and np.all(np.abs(_np(got.lse) - want[1]) <= tol[1])
