@@ -514,6 +514,7 @@ typedef struct {
  *   table_dev [table_rows][rot] float
  *   q_out_dev, k_out_dev: may be q_dev and k_dev with the same strides, else
  *       they overlap no input
+ *       (heads lie within rows or rows within heads: nothing is written twice)
  * Pointers but positions_dev must be 16-byte aligned.
  */
 paep_status paep_rotate(const paep_rotate_desc *desc, const void *q_dev, const void *k_dev,

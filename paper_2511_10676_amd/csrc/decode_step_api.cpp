@@ -81,7 +81,9 @@ paep_status check_rows(long long row, long long head, int n, int H, int width, i
     if (H > 1 && head < width) return PAEP_ERR_SHAPE;
     if (n > 1 && out && row < width) return PAEP_ERR_SHAPE;
     const int per16 = 16 / element_bytes(dtype);
-    return row % per16 || head % per16 ? PAEP_ERR_ALIGN : PAEP_OK;
+    if (row % per16 || head % per16) return PAEP_ERR_ALIGN;
+    // heads within rows, or rows within heads
+    return out && n > 1 && H > 1 && row < (H - 1) * head + width && (__int128)head < (__int128)(n - 1) * row + width ? PAEP_ERR_SHAPE : PAEP_OK;
 }
 
 paep_status check_rotate(const paep_rotate_desc* d, bool append)

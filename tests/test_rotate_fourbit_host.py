@@ -54,6 +54,15 @@ def test_rotate_refuses_bad_arguments(append):
     assert _rotate(append, n=0, q=None, k=None, v=None, qo=None, ko=None, pos=None, pt=None) == OK
 
 
+def test_rotate_refuses_outputs_that_overlap():
+    assert _rotate(q_out_row_stride=64, q_out_head_stride=64) == E_SHAPE              # a row's second head on the next row's first
+    assert _rotate(k_out_row_stride=64, k_out_head_stride=64) == E_SHAPE
+    assert _rotate(n=1 << 24, q_out_row_stride=HUGE, q_out_head_stride=HUGE) == E_SHAPE
+    assert _rotate(q_out_row_stride=64, q_out_head_stride=128, k_out_row_stride=64, k_out_head_stride=128, n=0) == OK
+    for rows, heads in ((256, 64), (64, 128)):                                         # heads within rows, rows within heads: not refused for that
+        assert _rotate(q_out_row_stride=rows, q_out_head_stride=heads, table=None) == E_NULL
+
+
 def test_rotate_alone_refuses_bad_outputs_of_keys():
     assert _rotate(ko=None) == E_NULL and _rotate(ko=ODD) == E_ALIGN
     assert _rotate(k_out_row_stride=0) == E_SHAPE and _rotate(k_out_head_stride=68) == E_ALIGN
