@@ -13,7 +13,7 @@
 // (One workgroup for 512 positions of each sequence took 137 us for 31 sequences of 2000 to 32768 positions, 8 heads: half of it
 // before the first product and behind the last.)
 // What bounds it: a position of 128 + 128 dimensions is 136 bytes, 17 / 64 of bf16 storage.  Those 31 sequences, 380 MB, take 96 us
-// (4.0 TB/s), and with the products left out 94: reading 64-byte rows of 3000 streams; from a cache that fits on the chip 66 us.  131071
+// (4.0 TB/s), and and with the products left out as long: reading 64-byte rows of 3000 streams; pages that stay on the chip some 65 us.  131071
 // positions of 4 heads, 71 MB, 19 us, 5 of them before the first product and behind the last, and 9.7 us of join.  Rows fetched
 // through LDS, so that neighbouring lanes read neighbouring bytes, or two tiles ahead, take as long.
 #include <type_traits>
