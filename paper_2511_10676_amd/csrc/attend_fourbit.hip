@@ -32,6 +32,9 @@ static constexpr int UNIT = FOUR_WAVES * FOUR_TILE;          // of a workgroup: 
 static constexpr int LEAST_UNITS = 2, ENOUGH_UNITS = 16, ENOUGH_SPANS = 512, MOST_SPANS = 2304;
 static constexpr int SEQUENCES = 1024;           // of a launch
 static constexpr float LOG2E_REST = 1.92596303e-8f;          // log2 e - LOG2E
+// Scores in units of log2 up to this are right.  A reference point is such a score rounded, and the exponentials, of what fmaf has unrounded,
+// and `rest` below carry a power of 2 that grows with that rounding: less than 4 up to here, past fp32's range from 2^31 on.
+static constexpr float FARTHEST = 0x1p24f;
 
 struct FourPlan {
     int G, head_blocks;          // query heads of a key-value head, blocks of 16 of them
@@ -456,8 +459,8 @@ void attend_fourbit_kernel(AttendFourbitArgs a, FourPlan pl)
             for (int w = 0; w < FOUR_WAVES; ++w) whole_sum += wave_l[w][m] * power(wave_m[w][m] - origin(all));
             const float mine = power(top - origin(all));
             const float by = whole_sum == 0.0f ? 0.0f : 1.0f / whole_sum;    // no position, or none above -infinity: zeros
-            // no weight at all: scores past the range of this form
-            bool odd = begin < end && !(whole_sum > 0.0f);
+            // no weight at all, or scores past the range of this form
+            bool odd = begin < end && (!(whole_sum > 0.0f) || fabsf(all) > FARTHEST);
             if (wave == 0 && g == 0 && h < pl.G) {
                 // the reference point as a natural exponent; what its rounding leaves goes into the sum
                 const float ref = SPECIAL || all == -__builtin_inff() ? all : all * LN2;
@@ -512,8 +515,8 @@ void attend_fourbit_kernel(AttendFourbitArgs a, FourPlan pl)
             return odd;
         };
         // Scores in units of log2 may be past the largest number where they are not, and the sum over up to 2^31 values may where their
-        // average is not: a piece whose results are not finite, or that has no weight, is done again, with scores as they are and 2^-32
-        // of each term.
+        // average is not: a piece whose results are not finite, that has no weight, or whose scores are past FARTHEST, is done again, with
+        // scores as they are and 2^-32 of each term.
         const bool odd = run(std::false_type{});
         if (__builtin_expect(__syncthreads_or(odd), 0)) run(std::true_type{});
     }
