@@ -254,8 +254,7 @@ void attend_fourbit_kernel(AttendFourbitArgs a, FourPlan pl)
             constexpr bool SPECIAL = decltype(special_c)::value;
             constexpr float unit = SPECIAL ? 0x1p-32f : 1.0f;    // what an exponential of 0 counts as
             constexpr float NEAR = SPECIAL ? 8.0f : 8.0f * LOG2E;
-            // (above 0: where the scale is 0, a row that does not take part has a score of -infinity all the same)
-            const float by_scale = fmaxf(SPECIAL ? scale : scale * LOG2E, 0x1p-126f);
+            const float by_scale = SPECIAL ? scale : scale * LOG2E;
             auto power = [&](float v) { return SPECIAL ? exp_(v) : __builtin_amdgcn_exp2f(v); };       // of differences of scores
             f32x4 o[VD];
             float top = -__builtin_inff(), sum = 0.0f;           // the exponentials' reference point
@@ -356,7 +355,7 @@ void attend_fourbit_kernel(AttendFourbitArgs a, FourPlan pl)
 
                     float z[8], most;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) z[j] = s[j >> 2][j & 3];
+                    for (int j = 0; j < 8; ++j) z[j] = SPECIAL ? s[j >> 2][j & 3] * by_scale : s[j >> 2][j & 3];
                     if (!whole) {
                         // what stands in a row that does not take part may be anything: no NaN of it may reach the sums
 #pragma unroll
@@ -365,9 +364,6 @@ void attend_fourbit_kernel(AttendFourbitArgs a, FourPlan pl)
                             t.vs[j >> 2] = (now >> j) & 1u ? t.vs[j >> 2] : (t.vs[j >> 2] & ~(255u << (8 * (j & 3)))) | 127u << (8 * (j & 3));
                         }
                     }
-                    if constexpr (SPECIAL)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) z[j] *= by_scale;
                     most = fmaxf(fmaxf(z[0], z[1]), z[2]);
 #pragma unroll
                     for (int j = 3; j < 8; ++j) most = fmaxf(most, z[j]);
@@ -516,8 +512,9 @@ void attend_fourbit_kernel(AttendFourbitArgs a, FourPlan pl)
         };
         // Scores in units of log2 may be past the largest number where they are not, and the sum over up to 2^31 values may where their
         // average is not: a piece whose results are not finite, that has no weight, or whose scores are past FARTHEST, is done again, with
-        // scores as they are and 2^-32 of each term.
-        const bool odd = run(std::false_type{});
+        // scores as they are and 2^-32 of each term.  That is the only way where the scale is below the normal numbers: by 0 the scores of
+        // rows that take part are equal, and those of the others have to be -infinity all the same.
+        const bool odd = scale < 0x1p-126f || run(std::false_type{});
         if (__builtin_expect(__syncthreads_or(odd), 0)) run(std::true_type{});
     }
 }

@@ -104,3 +104,38 @@ def test_equal_scores_of_any_size(kind, ps):
                 assert np.all(np.abs(out[b] - v.mean(axis=0)) <= tol), (scale, size, n)
                 off = (PARTS[kind] * 64 + 1 + 6) * U * np.abs(score[b]) + ((n + 16) * 2 + 4 * np.log(n)) * U
                 assert np.all(np.abs(lse[b] - score[b] - np.log(n)) <= off), (scale, size, n)
+
+
+@pytest.mark.parametrize("ps", [16, 4])
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_scales_of_zero_and_next_to_it(kind, ps):
+    """Products up to 1e38: by 0 they are equal; by numbers too small to be normal ones they are scores of size 1e-2 to 1e-7."""
+    g = torch.Generator(device="cuda").manual_seed(33)
+    for pattern in ("above", "zeros", "below"):
+        r = Rows(g, ps, pattern=pattern)
+        q = _queries(g, 1e38, 1.0, kind, len(r.lengths))
+        k = R.values(r.kp.cpu().numpy(), r.ks.transpose(2, 3).cpu().numpy())
+        for scale in (0.0, -0.0, 1e-40, -1e-40, 1e-45):
+            out, lse = r.attend(q, scale)
+            want, tol = R.attend(_np(q), k, r.v, r.table.cpu().numpy(), r.lengths, None, float(np.float32(scale)), r.table.shape[1] * ps, kind)
+            assert np.all(np.abs(out - want[0]) <= tol[0]) and np.all(np.abs(lse - want[1]) <= tol[1]), (pattern, scale)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_scales_of_zero_and_next_to_it_over_rows_that_are_left_out(kind):
+    """Rows before the start, behind the end and on pages that are none take no part, whatever the scale."""
+    g = torch.Generator(device="cuda").manual_seed(34)
+    for ps in (16, 4):
+        r = Rows(g, ps, n=(300, 37, 5))
+        r.table[0, 2] = -1
+        r.vs.fill_(127)
+        lens, starts = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ((300, 37, 5), (21, 36, 5)))
+        v = R.values(r.vp.cpu().numpy(), r.vs.transpose(2, 3).cpu().numpy())
+        k = R.values(r.kp.cpu().numpy(), r.ks.transpose(2, 3).cpu().numpy())
+        q = _queries(g, 1e38, 1.0, kind, 3)
+        for scale in (0.0, 1e-40):
+            got = B.attend_fourbit(q, r.kp, r.vp, r.ks, r.vs, r.table, lens, starts=starts, scale=scale, want_lse=True)
+            want, tol = R.attend(_np(q), k, v, r.table.cpu().numpy(), [300, 37, 5], [21, 36, 5], float(np.float32(scale)), r.table.shape[1] * ps, kind)
+            assert np.all(np.abs(_np(got.out) - want[0]) <= tol[0])
+            lse = _np(got.lse)
+            assert np.all(lse[2] == -np.inf) and np.all(np.abs(lse[:2] - want[1][:2]) <= tol[1][:2])
