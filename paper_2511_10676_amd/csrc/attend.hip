@@ -36,6 +36,27 @@ static constexpr int ATT_THREADS = 256, ATT_WAVES = ATT_THREADS / 64;
 static constexpr int TILE = 16;                  // positions of a wave at a time
 static constexpr int TABLE = 2048;               // page-table entries in LDS at a time
 
+struct AttendPlan {
+    int G, head_blocks;          // query heads of a key-value head, blocks of 16 of them
+    int chunk, S;                // positions of a workgroup, chunks of the longest sequence
+    int rows;                    // B * Hkv
+    float* o;                    // [rows][S][G][Dv] outputs of the chunks, each over its own sum (S > 1)
+    float2* ml;                  // [rows][S][G] the maxima of their scores, and their sums (S > 1 or mass)
+    float* scores;               // [rows][S][G][chunk] (mass)
+};
+
+// the part of a sequence that is looked at: positions start .. len, counted in chunks from start rounded down to a multiple of 16
+struct Range { int start, first, len, chunks; };
+__device__ __forceinline__ Range range_of(const int32_t* lengths, const int32_t* starts, int b, int max_len, int chunk)
+{
+    Range r;
+    r.len = clamped_length(lengths, b, max_len);
+    r.start = starts && starts[b] > 0 ? starts[b] : 0;
+    r.first = r.start & ~15;
+    r.chunks = r.start < r.len ? (int)(((uint32_t)(r.len - r.first) + (uint32_t)chunk - 1) / (uint32_t)chunk) : 0;
+    return r;
+}
+
 // 16 x 16 products of two operands of 16 rows x 64 bytes
 template <bool BF16> __device__ __forceinline__ f32x4 product(const u32x4& x, const u32x4& y, f32x4 acc)
 {
@@ -451,26 +472,26 @@ __global__ __launch_bounds__(JOIN_THREADS) void attend_join_kernel(AttendArgs a,
 // sequences a chunk has at most 512 positions, because their lengths differ and the host does not know them (61 sequences of
 // 17 to 8192 positions with mass: 105 us, 129 in chunks of 2048; where the lengths are equal it costs: 61 of 1400 each 80 us, and
 // 66 in one chunk each); one sequence is cut into chunks of up to 2048.
-static constexpr AttendCut CUT = {512, 256, ATT_WAVES * TILE, 2048, 512};
-
-// the most positions of a chunk: as the cut says, and 1 / 256 of the longest where that is more
-static long long longest_chunk(const AttendArgs& a, const AttendCut& cut)
+static constexpr int TARGET = 512, LEAST = 256;      // workgroups; positions of a chunk
+static constexpr int STEP = ATT_WAVES * TILE;        // positions that a workgroup's waves take at once
+// the most positions of a chunk: 2048, 512 where there are several sequences, and 1 / 256 of the longest where that is more
+static long long longest_chunk(const AttendArgs& a)
 {
-    const long long most = a.c.B > 1 ? cut.most_several : cut.most_alone, share = (a.max_len + 255ll) / 256;
+    const long long most = a.c.B > 1 ? 512 : 2048, share = (a.max_len + 255ll) / 256;
     return most > share ? most : share;
 }
-AttendPlan attend_plan(const AttendArgs& a, const AttendCut& cut)
+static AttendPlan plan_of(const AttendArgs& a)
 {
     AttendPlan pl{};
     pl.G = a.Hq / a.c.Hkv;
     pl.head_blocks = (pl.G + 15) / 16;
     pl.rows = a.c.B * a.c.Hkv;
     const long long items = pl.rows > 0 ? (long long)pl.rows * pl.head_blocks : 1;
-    long long chunk = ((long long)a.max_len * items + cut.target - 1) / cut.target;
-    if (chunk > longest_chunk(a, cut)) chunk = longest_chunk(a, cut);
-    if (chunk < cut.least) chunk = cut.least;
+    long long chunk = ((long long)a.max_len * items + TARGET - 1) / TARGET;
+    if (chunk > longest_chunk(a)) chunk = longest_chunk(a);
+    if (chunk < LEAST) chunk = LEAST;
     if (chunk > a.max_len + 16ll) chunk = a.max_len + 16ll;      // a first position is rounded down
-    pl.chunk = (int)((chunk + cut.step - 1) / cut.step * cut.step);
+    pl.chunk = (int)((chunk + STEP - 1) / STEP * STEP);
     pl.S = (int)((a.max_len + 15ll + pl.chunk - 1) / pl.chunk);
     if (pl.S < 1) pl.S = 1;
     return pl;
@@ -478,10 +499,10 @@ AttendPlan attend_plan(const AttendArgs& a, const AttendCut& cut)
 
 static size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 
-bool attend_plan_fits(const AttendArgs& a, const AttendCut& cut)
+bool attend_fits(const AttendArgs& a)
 {
     if ((long long)a.c.B * a.c.Hkv >= (1ll << 23) || (long long)a.c.B * a.Hq >= (1ll << 23)) return false;
-    const AttendPlan pl = attend_plan(a, cut);
+    const AttendPlan pl = plan_of(a);
     const long long wgs = ((long long)pl.rows * pl.S + 7) * pl.head_blocks;
     const long long join = (long long)a.c.B * a.Hq + (a.mass ? (long long)pl.rows * ((a.max_len + 15ll) / MASS_POSITIONS + 1) : 0);
     return wgs < (1ll << 23) && join < (1ll << 23);              // a launch's threads stay below 2^32
@@ -489,50 +510,25 @@ bool attend_plan_fits(const AttendArgs& a, const AttendCut& cut)
 
 // Enough for this call and for every one with a smaller max_len, B or Hkv (of the same G): the number of chunks falls where their
 // size grows by a step, so what is counted here are bounds that only grow.  For unrounded chunks of c positions,
-//   c >= least                              chunks of all heads <= heads * ceil((max_len + 15) / least)
-//   c = max_len * items / target            <= target * (query heads of an item) + 2 heads
+//   c >= LEAST                              chunks of all heads <= heads * ceil((max_len + 15) / LEAST)
+//   c = max_len * items / TARGET            <= TARGET * (query heads of an item) + 2 heads
 //   c = longest_chunk                       <= heads * ceil((max_len + 15) / c), and never more than 258 of a head
-// and a head's chunks have less than max_len + 15 + c positions together, c <= longest_chunk, max_len + 16, rounded to a step.
-size_t attend_plan_workspace(const AttendArgs& a, const AttendCut& cut)
+// and a head's chunks have less than max_len + 15 + c positions together, c <= longest_chunk, max_len + 16, rounded to STEP.
+size_t attend_workspace_bytes(const AttendArgs& a)
 {
-    const AttendPlan pl = attend_plan(a, cut);
+    const AttendPlan pl = plan_of(a);
     const size_t heads = (size_t)a.c.B * a.Hq, positions = (size_t)a.max_len + 15;
     auto least = [](size_t x, size_t y) { return x < y ? x : y; };
     auto most = [](size_t x, size_t y) { return x > y ? x : y; };
     auto chunks_of = [&](size_t c) { return (positions + c - 1) / c; };
-    const size_t parts = least(heads * chunks_of(cut.least), most(((size_t)cut.target * pl.G + pl.head_blocks - 1) / pl.head_blocks + 2 * heads,
-                                                                  heads * least(chunks_of(a.c.B > 1 ? cut.most_several : cut.most_alone), 258)));
+    const size_t parts = least(heads * chunks_of(LEAST), most(((size_t)TARGET * pl.G + pl.head_blocks - 1) / pl.head_blocks + 2 * heads,
+                                                              heads * least(chunks_of(a.c.B > 1 ? 512 : 2048), 258)));
     size_t n = 0;
-    if (chunks_of(cut.least) > 1) n += up16(parts * a.c.Dv * 4);
-    if (chunks_of(cut.least) > 1 || a.mass) n += up16(parts * 8);
-    if (a.mass) n += heads * (positions + least(most(longest_chunk(a, cut), cut.least), positions + 1) + cut.step) * 4;
+    if (chunks_of(LEAST) > 1) n += up16(parts * a.c.Dv * 4);
+    if (chunks_of(LEAST) > 1 || a.mass) n += up16(parts * 8);
+    if (a.mass) n += heads * (positions + least(most(longest_chunk(a), LEAST), positions + 1) + STEP) * 4;
     return heads ? n : 0;
 }
-
-AttendPlan attend_plan_placed(const AttendArgs& a, const AttendCut& cut)
-{
-    AttendPlan pl = attend_plan(a, cut);
-    const size_t parts = (size_t)a.c.B * a.Hq * pl.S;
-    unsigned char* ws = (unsigned char*)a.workspace;
-    if (pl.S > 1) { pl.o = (float*)ws; ws += up16(parts * a.c.Dv * 4); }
-    if (pl.S > 1 || a.mass) { pl.ml = (float2*)ws; ws += up16(parts * 8); }
-    if (a.mass) pl.scores = (float*)ws;
-    return pl;
-}
-
-hipError_t launch_attend_join(const AttendArgs& a, const AttendPlan& pl)
-{
-    const int joins = pl.S > 1 ? a.c.B * a.Hq : 0;
-    const int mass_blocks = a.mass ? (int)((a.max_len + 15ll) / MASS_POSITIONS + 1) : 0;
-    const long long wgs = joins + (long long)pl.rows * mass_blocks;
-    if (wgs == 0) return hipSuccess;
-    hipLaunchKernelGGL((a.c.dtype == 1 ? attend_join_kernel<true> : attend_join_kernel<false>), dim3((unsigned)wgs), dim3(JOIN_THREADS), 0,
-                       a.stream, a, pl, joins, mass_blocks);
-    return hipGetLastError();
-}
-
-bool attend_fits(const AttendArgs& a) { return attend_plan_fits(a, CUT); }
-size_t attend_workspace_bytes(const AttendArgs& a) { return attend_plan_workspace(a, CUT); }
 
 template <bool BF16> static hipError_t launch(const AttendArgs& a, const AttendPlan& pl)
 {
@@ -545,13 +541,23 @@ template <bool BF16> static hipError_t launch(const AttendArgs& a, const AttendP
                              : (wide ? attend_kernel<BF16, 8 * W, 2 * W, MASS> : attend_kernel<BF16, 8 * W, W, MASS>);
     };
     hipLaunchKernelGGL((a.mass ? kern(std::true_type{}) : kern(std::false_type{})), dim3((unsigned)((pl.rows * pl.S + 7) / 8 * 8 * pl.head_blocks)), dim3(ATT_THREADS), 0, a.stream, a, pl);
-    const hipError_t err = hipGetLastError();
-    return err != hipSuccess ? err : launch_attend_join(a, pl);
+    hipError_t err = hipGetLastError();
+    const int joins = pl.S > 1 ? a.c.B * a.Hq : 0;
+    const int mass_blocks = a.mass ? (int)((a.max_len + 15ll) / MASS_POSITIONS + 1) : 0;
+    const long long wgs = joins + (long long)pl.rows * mass_blocks;
+    if (err != hipSuccess || wgs == 0) return err;
+    hipLaunchKernelGGL(attend_join_kernel<BF16>, dim3((unsigned)wgs), dim3(JOIN_THREADS), 0, a.stream, a, pl, joins, mass_blocks);
+    return hipGetLastError();
 }
 
 hipError_t launch_attend(const AttendArgs& a)
 {
-    const AttendPlan pl = attend_plan_placed(a, CUT);
+    AttendPlan pl = plan_of(a);
+    const size_t parts = (size_t)a.c.B * a.Hq * pl.S;
+    unsigned char* ws = (unsigned char*)a.workspace;
+    if (pl.S > 1) { pl.o = (float*)ws; ws += up16(parts * a.c.Dv * 4); }
+    if (pl.S > 1 || a.mass) { pl.ml = (float2*)ws; ws += up16(parts * 8); }
+    if (a.mass) pl.scores = (float*)ws;
     return a.c.dtype == 1 ? launch<true>(a, pl) : launch<false>(a, pl);
 }
 
