@@ -624,7 +624,7 @@ __global__ __launch_bounds__(FOUR_JOIN_THREADS) void attend_fourbit_join_kernel(
     __syncthreads();
     // thread (lane, i): two neighbouring dimensions, (4g + i) * VD + 2 group ..
     const int d = (4 * (lane >> 4) + wave) * VD + group * 2;
-    if (wave >= 4 || h >= pl.G || d >= a.a.c.Dv) return;
+    if (h >= pl.G || d >= a.a.c.Dv) return;
     float out[2] = {};
 #pragma unroll
     for (int w = 0; w < FOUR_JOIN_WAVES; ++w)
