@@ -13,9 +13,9 @@
 // (One workgroup for 512 positions of each sequence took 137 us for 31 sequences of 2000 to 32768 positions, 8 heads: half of it
 // before the first product and behind the last.)
 // What bounds it: a position of 128 + 128 dimensions is 136 bytes, 17 / 64 of bf16 storage.  Those 31 sequences, 380 MB, take 96 us
-// (4.0 TB/s), and and with the products left out as long: reading 64-byte rows of 3000 streams; pages that stay on the chip some 65 us.  131071
-// positions of 4 heads, 71 MB, 19 us, 5 of them before the first product and behind the last, and 9.7 us of join.  Rows fetched
-// through LDS, so that neighbouring lanes read neighbouring bytes, or two tiles ahead, take as long.
+// (4.0 TB/s), and as long with the products left out: what bounds them is reading 64-byte rows of 3000 streams, and with pages that stay
+// on the chip they take some 65 us.  131071 positions of 4 heads, 71 MB, 19 us, 5 of them before the first product and behind the last, and
+// 9.7 us of join.  Rows fetched through LDS, so that neighbouring lanes read neighbouring bytes, or two tiles ahead, take as long.
 #include <type_traits>
 
 #include "attend_device.h"
@@ -27,8 +27,9 @@ static constexpr int FOUR_THREADS = 256, FOUR_WAVES = FOUR_THREADS / 64;
 static constexpr int FOUR_TILE = 32;             // positions of a wave at a time, two halves of 16
 static constexpr int UNIT = FOUR_WAVES * FOUR_TILE;          // of a workgroup: what spans are counted in
 // A span has at least 2 units, and more where that leaves 512 spans, two for every CU; from 16 units on there are as many spans as
-// that gives, up to 2304 (61 sequences of 1400 positions, 8 heads: 31 us, with 8 in place of the 16, which cuts every sequence,
-// 45; 131071 positions of 4 heads: 32 us, for 768 spans 37; 31 long sequences: 118 us, with 8 123, for 1536 or 4096 spans the same).
+// that gives, up to 2304 (times of both launches: 61 sequences of 1400 positions, 64 query heads of 8: 31 us, with 8 in place of the 16,
+// which cuts every sequence, 50; 31 of 2000 to 32768 positions: 116.5 us, with 8 119, for 768 spans 118, 1536 115.5, 4096 116.4; one of
+// 131071 positions, 4 heads: 28.5 us, with 8 28.6, for 768 to 4096 spans 28.2 to 28.4).
 static constexpr int LEAST_UNITS = 2, ENOUGH_UNITS = 16, ENOUGH_SPANS = 512, MOST_SPANS = 2304;
 static constexpr int SEQUENCES = 1024;           // of a launch
 static constexpr float LOG2E_REST = 1.92596303e-8f;          // log2 e - LOG2E
@@ -99,7 +100,9 @@ template <int W> __device__ __forceinline__ void load_own(const unsigned char* a
 }
 
 // QP: bf16 parts of a query element (1: bf16 storage, 3: fp32); KW: 4-byte words of a key in a lane (16 lanes' worth of 4 words
-// cover 128 dimensions); VD: dimensions of a value in a lane; PAGED16: 16 neighbours are on one page, whose address is the wave's
+// cover 128 dimensions); VD: dimensions of a value in a lane; PAGED16: 16 neighbours are on one page, whose address is the
+// wave's (else every lane looks up its rows' pages, one load behind the other; pages of 16 or 64 and of 8 positions: the 31 sequences
+// above 116.5 and 209 us, the one of 131071 28.5 and 42, 61 of 1400 31 and 54)
 template <int QP, int KW, int VD, bool PAGED16>
 __global__ __launch_bounds__(FOUR_THREADS, KW <= 4 && VD <= 8 && QP == 1 && PAGED16 ? 3 : KW == 8 && QP == 3 ? 1 : 2)
 void attend_fourbit_kernel(AttendFourbitArgs a, FourPlan pl)

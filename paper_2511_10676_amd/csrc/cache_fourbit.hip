@@ -147,8 +147,10 @@ __global__ __launch_bounds__(CELL_THREADS) void read_fourbit_kernel(
 }
 
 // Calls `launch(tokens of a thread, first token, end, cells)` for parts whose threads stay below 2^31.  A thread works on several tokens
-// where there are enough of them to fill the device: finding its place among heads and pieces is most of what it computes
-// (8192 tokens of 8 heads of 128 + 128: append 14.5 -> 11.3 us, 3.8 TB/s, read 14.3 -> 11.4).
+// where there are enough of them to fill the device: finding its place among heads and pieces is most of what it computes.  8 heads of
+// 128 + 128, us for one token of a thread and for four, append; read.  bf16: 8192 tokens 15.3, 11.7 (3.6 TB/s); 14.5, 11.7.  4096, the
+// switch: 9.6, 8.5; 9.4, 8.4.  2048: 6.1, 5.6; 5.8, 5.6.  1024: 4.5, 4.7; 4.4, 4.7.  fp32: 16384 tokens 37.5, 35.7; 46.4, 48.8.
+// 8192: 16.3, 15.8; 19.1, 20.0.  4096: 10.3, 10.1; 11.9, 11.9.  2048: 7.0, 7.4; 8.0, 8.2.
 static constexpr int SEVERAL = 4;
 template <typename F> static hipError_t in_parts(const CacheView& c, int n, F launch)
 {

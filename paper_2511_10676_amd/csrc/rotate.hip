@@ -9,6 +9,8 @@
 // goes from lane to lane.  Where pairs do not fill pieces, a row goes through LDS.
 // Measured: 8191 bf16 tokens of 36 heads of 128, with norms, 151 MB, 27 us (5.6 TB/s); 4096 fp32 tokens of 27 heads of 80 into a cache,
 // 71 MB, 16 us (4.6 TB/s); 61 tokens of 48 heads 4.1 us, one token 2.1 us, a launch.
+// Through LDS, where each element reads a cosine, a sine and its other half: 8191 bf16 tokens of 36 heads of 80, 40 of their dimensions
+// rotated, 59 us, 27 for all 80 (not through LDS); 4096 fp32 tokens, 20 dimensions, 33 us, 24 for all.
 #include <type_traits>
 
 #include "cache_device.h"
@@ -185,8 +187,12 @@ hipError_t launch_rotate(const RotateArgs& a)
     int log_lanes = 0;
     while ((2 * per << log_lanes) < widest) ++log_lanes;
     const bool lds = a.rot % (2 * per) != 0;                 // pairs that do not fill pieces
-    // Outputs of many tokens leave the caches alone where a row's lanes write whole cache lines together (8191 tokens of 36 heads of
-    // 128, 75 MB out: 33.5 -> 26.5 us; where they write every second 16 bytes it takes longer, 4096 fp32 tokens into a cache 16.4 -> 22.2).
+    // Outputs of many tokens leave the caches alone where a row's lanes write whole cache lines together (where they write every
+    // second 16 bytes it takes longer, 4096 fp32 tokens into a cache 16.4 -> 22.2 us).  Heads of 128, through the caches and past them, alone,
+    // and with a copy of all queries behind it, which then has to fetch them from memory (the rule goes by the call alone):
+    //   19 MB out: 10.7, 9.8 us; 16.5, 17.3        38 MB: 16.6, 16.1; 30.8, 32.3        57 MB: 27.6, 22.4; 46.0, 47.7
+    //   67 MB: 32.2, 25.6; 51.0, 55.5              75 MB: 35.4, 28.0; 55.9, 61.0
+    //   151 MB: 62.7, 57.9; 122, 111               302 MB: 118, 111; 216, 214
     const bool stream = !append && !lds && a.style == 0 && a.rot == a.D && a.D * 16 / per >= 256 &&
                         (long long)a.n * (a.Hq + a.Hk) * a.D * 16 / per >= (64ll << 20);
     auto kern = bf16 ? (append ? (lds ? rotate_kernel<true, true, true, false> : rotate_kernel<true, true, false, false>)
